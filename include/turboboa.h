@@ -302,6 +302,85 @@ tb_status tb_unpack_dequant(const unsigned int* packed, const float* scales, con
                             unsigned long long* mismatch, void* stream);
 
 /* --------------------------------------------------------------------------
+ * Products with bit-packed weights: what runs a quantized projection, and what
+ * fine-tunes low-rank adapters beside it.  No counterpart in the paper, whose
+ * method ends with Q = diag(s)(W_int - z).
+ * -------------------------------------------------------------------------- */
+
+/* A projection as tb_pack_codes and tb_quantize_layer leave it. */
+typedef struct {
+  int d_out, d_in;            /* d_out a multiple of 8, d_in a multiple of 32       */
+  int bits;                   /* 2..8                                               */
+  int quant_group;            /* 0 = the whole row, else a multiple of 32 that
+                                 divides d_in                                       */
+  const unsigned int* packed; /* [d_out][d_in * bits / 32], 16-byte aligned         */
+  const float* scales;        /* [d_out][n_g]                                       */
+  const int* zeros;           /* [d_out][n_g]; -128 .. 255 on the tensor-core paths
+                                 (the quantizer's lie in 0 .. 2^bits - 1): beyond,
+                                 code - zero is rounded to bf16's eight bits        */
+} tb_packed_weight;
+
+/* Low-rank adapters of the requests in a batch.  Request j has the tokens starts[j] ..
+ * starts[j + 1] - 1 and adapter ids[j]; an id outside 0 .. n_adapters - 1 means none, and
+ * so does a token of no request (before starts[0], from starts[n_requests] on).  starts
+ * must not decrease; requests may be empty and may share adapters.  Adapter i adds
+ * scale[i] (x A_i^T) B_i to the projection: both matrices are stored [rank][width], so
+ * that the forward and the backward pass read them alike. */
+typedef struct {
+  int n_adapters, rank;       /* rank: a multiple of 8, 8..128 (pad with zero rows) */
+  int n_requests;
+  const void* A;              /* [n_adapters][rank][d_in], the activations' type, 16-byte aligned */
+  const void* B;              /* [n_adapters][rank][d_out], likewise                */
+  const float* scale;         /* [n_adapters]                                       */
+  const int* starts;          /* [n_requests + 1], device                           */
+  const int* ids;             /* [n_requests], device                               */
+} tb_adapters;
+
+/* y = x Q^T, plus the adapters' share where `adapters` is not NULL.
+ *   x  [n_tok][d_in], y [n_tok][d_out]: bf16 or float (x_type), 16-byte aligned
+ *   xa [n_tok][rank] float, required with adapters: x_t A_i^T of every token, not
+ *      scaled, zero for a token without an adapter; the backward pass takes it
+ * Sums are float and are rounded to the type of y once.  A value that is not finite
+ * reaches the outputs of its own token alone, and one in an adapter those of its requests.
+ * n_tok may be 0.  Workspace: tb_packed_linear_workspace bytes (may be 0). */
+size_t tb_packed_linear_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
+                                  tb_dtype x_type, long long n_tok);
+tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapters, const void* x,
+                           tb_dtype x_type, long long n_tok, void* y, float* xa, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* Gradients of tb_packed_linear with respect to its input and the adapters; the packed
+ * weight is a constant.  With u_t = scale[i] dy_t B_i^T:
+ *   dx  [n_tok][d_in] of x_type, or NULL:  dx = dy Q + u_t A_i
+ *   dA  [n_adapters][rank][d_in] float:    dA_i = sum of u_t^T x_t over i's tokens
+ *   dB  [n_adapters][rank][d_out] float:   dB_i = sum of scale[i] xa_t^T dy_t
+ * dA and dB come together or are both NULL; they are overwritten (zeros for an adapter
+ * that no token has), the same bits on every call.  The input comes as x, in full, or
+ * as x_codes and x_scales from tb_checkpoint_pack; xa is the forward pass's.  x, codes
+ * and xa may be NULL without dA.  dy [n_tok][d_out] of x_type.
+ * In bf16 the weights enter dx rounded to bf16. */
+size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
+                                           tb_dtype x_type, long long n_tok);
+tb_status tb_packed_linear_backward(const tb_packed_weight* w, const tb_adapters* adapters,
+                                    const void* dy, tb_dtype x_type, long long n_tok, const void* x,
+                                    const signed char* x_codes, const float* x_scales,
+                                    const float* xa, void* dx, float* dA, float* dB, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Activations kept in 8 bits between the passes: every token and run of 128 columns (the
+ * last one may be shorter) has scale = max|x| / 127, rounded to float once, and codes
+ * rne(x / scale) in -127 .. 127 of the true quotient; a run of zeros has scale 0, a run with a value that is
+ * not finite has a scale that is no number, and so have its values.
+ *   x      [n_tok][d] bf16 or float, d a multiple of 32; 16-byte aligned
+ *   codes  [n_tok][d] signed char, 16-byte aligned
+ *   scales [n_tok][(d + 127) / 128] float
+ * tb_checkpoint_unpack writes code * scale, rounded to x_type. */
+tb_status tb_checkpoint_pack(const void* x, tb_dtype x_type, long long n_tok, int d,
+                             signed char* codes, float* scales, void* stream);
+tb_status tb_checkpoint_unpack(const signed char* codes, const float* scales, long long n_tok,
+                               int d, tb_dtype x_type, void* x, void* stream);
+
+/* --------------------------------------------------------------------------
  * Block level: Algorithm 1's outer loop over the projections of an attention
  * layer.
  * -------------------------------------------------------------------------- */

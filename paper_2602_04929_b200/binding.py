@@ -80,6 +80,12 @@ _SIGNATURES = {
     "tb_packed_bytes": (_sz, [_int, _int, _int]),
     "tb_pack_codes": (_int, [_vp, _int, _int, _int, _vp, _vp]),
     "tb_unpack_dequant": (_int, [_vp, _vp, _vp, _int, _int, _int, _int, _vp, _vp, _vp, _vp, _f, _vp, _vp]),
+    "tb_packed_linear_workspace": (_sz, [_vp, _vp, _int, _ll]),
+    "tb_packed_linear": (_int, [_vp, _vp, _vp, _int, _ll, _vp, _vp, _vp, _sz, _vp]),
+    "tb_packed_linear_backward_workspace": (_sz, [_vp, _vp, _int, _ll]),
+    "tb_packed_linear_backward": (_int, [_vp, _vp, _vp, _int, _ll] + [_vp] * 8 + [_sz, _vp]),
+    "tb_checkpoint_pack": (_int, [_vp, _int, _ll, _int, _vp, _vp, _vp]),
+    "tb_checkpoint_unpack": (_int, [_vp, _vp, _ll, _int, _int, _vp, _vp]),
     "tb_profile_enable": (None, [_int]),
     "tb_profile_read": (_int, [ctypes.POINTER(ctypes.c_double), _int]),
     "tb_quantize_from_host_workspace": (_sz, [ctypes.POINTER(LayerDesc), _ll, _int]),
@@ -474,6 +480,154 @@ def tb_unpack_dequant(packed, scales, zeros, d_in: int, bits: int, quant_group: 
                                     _ptr(codes_ref, torch.uint8, True), _ptr(w_hat_ref, torch.float32, True), float(tol),
                                     _ptr(mism, None, True), _stream()), "tb_unpack_dequant")
     return codes, w_hat, mism
+
+
+class PackedWeight(ctypes.Structure):
+    """tb_packed_weight; holds the tensors it points to."""
+    _fields_ = [("d_out", ctypes.c_int), ("d_in", ctypes.c_int), ("bits", ctypes.c_int), ("quant_group", ctypes.c_int),
+                ("packed", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p)]
+
+
+class Adapters(ctypes.Structure):
+    """tb_adapters; holds the tensors it points to."""
+    _fields_ = [("n_adapters", ctypes.c_int), ("rank", ctypes.c_int), ("n_requests", ctypes.c_int), ("A", ctypes.c_void_p),
+                ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("ids", ctypes.c_void_p)]
+
+
+def packed_weight(packed, scales, zeros, d_in: int, bits: int, quant_group: int = 0) -> PackedWeight:
+    """A projection as tb_pack_codes and tb_quantize_layer leave it: packed words, scales, zero-points."""
+    n_g = d_in // quant_group if quant_group else 1
+    if packed.dim() != 2 or packed.shape[1] * 32 != d_in * bits:
+        raise ValueError("packed must be [d_out][d_in * bits / 32]")
+    for t in (scales, zeros):
+        if tuple(t.shape) != (packed.shape[0], n_g):
+            raise ValueError("scales and zeros must be [d_out][d_in / quant_group]")
+    w = PackedWeight(packed.shape[0], d_in, bits, quant_group, _ptr(packed, torch.int32), _ptr(scales, torch.float32),
+                     _ptr(zeros, torch.int32))
+    w.tensors = (packed, scales, zeros)
+    w.device = _one_device(w.tensors)
+    return w
+
+
+def adapters(A, B, scale, starts, ids) -> Adapters:
+    """Low-rank adapters A [n][rank][d_in] and B [n][rank][d_out] with a factor each, and the adapter of every request:
+    request j has the tokens starts[j] .. starts[j + 1] - 1 and adapter ids[j] (negative: none)."""
+    if A.dim() != 3 or B.dim() != 3 or A.shape[:2] != B.shape[:2] or A.dtype != B.dtype or tuple(scale.shape) != A.shape[:1]:
+        raise ValueError("adapters must be A [n][rank][d_in], B [n][rank][d_out] of one dtype and scale [n]")
+    if starts.dim() != 1 or ids.dim() != 1 or starts.shape[0] != ids.shape[0] + 1:
+        raise ValueError("starts must have one entry more than ids")
+    a = Adapters(A.shape[0], A.shape[1], ids.shape[0], _ptr(A), _ptr(B), _ptr(scale, torch.float32), _ptr(starts, torch.int32),
+                 _ptr(ids, torch.int32))
+    a.tensors = (A, B, scale, starts, ids)
+    a.device = _one_device(a.tensors)
+    return a
+
+
+def _one_device(tensors) -> int:
+    """The CUDA device of all of them."""
+    devices = {t.device.index for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError("tensors must live on one device")
+    return devices.pop()
+
+
+def _on_current(w, ad, *tensors) -> None:
+    """A call runs on the current device: everything it takes has to be there."""
+    cur = _current_device()
+    if w.device != cur or (ad is not None and ad.device != cur) or any(t is not None and t.device.index != cur for t in tensors):
+        raise ValueError("tensors must live on the current device")
+
+
+def _packed_call(w, ad, x, width, other):
+    """Checks of the activations and adapters of a call; (type, C pointers of w and ad)."""
+    if x.dim() != 2 or x.shape[1] != width:
+        raise ValueError(f"activations must be [n_tok][{width}]")
+    if ad is not None:
+        if ad.tensors[0].dtype != x.dtype:
+            raise ValueError("adapters must have the activations' dtype")
+        if (ad.tensors[0].shape[2], ad.tensors[1].shape[2]) != (w.d_in, w.d_out):
+            raise ValueError("adapters must be [n][rank][d_in] and [n][rank][d_out] of the projection")
+    return _xtype(x), ctypes.addressof(w), None if ad is None else ctypes.addressof(ad)
+
+
+def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=None, y=None, xa=None):
+    """(y, xa): y = x Q^T, plus the adapters' share; xa [n_tok][rank] is x A^T of every token's adapter, which the backward
+    pass takes (None without adapters)."""
+    xt, wp, ap = _packed_call(w, adapters, x, w.d_in, w.d_out)
+    n_tok = x.shape[0]
+    if y is None:
+        y = torch.empty((n_tok, w.d_out), dtype=x.dtype, device=x.device)
+    elif tuple(y.shape) != (n_tok, w.d_out):
+        raise ValueError("y must be [n_tok][d_out]")
+    if adapters is None:
+        xa = None
+    elif xa is None:
+        xa = torch.empty((n_tok, adapters.rank), dtype=torch.float32, device=x.device)
+    elif tuple(xa.shape) != (n_tok, adapters.rank):
+        raise ValueError("xa must be [n_tok][rank]")
+    _on_current(w, adapters, x, y, xa, ws)
+    lib = load()
+    if ws is None:
+        nbytes = lib.tb_packed_linear_workspace(wp, ap, xt, n_tok)
+        ws = _workspace(nbytes, x.device) if nbytes else None
+    _check(lib.tb_packed_linear(wp, ap, _ptr(x), xt, n_tok, _ptr(y, x.dtype), _ptr(xa, torch.float32, True),
+                                _ptr(ws, None, True), 0 if ws is None else ws.numel(), _stream()), "tb_packed_linear")
+    return y, xa
+
+
+def tb_packed_linear_backward(w: PackedWeight, dy, adapters: Adapters | None = None, x=None, checkpoint=None, xa=None,
+                              want_dx: bool = True, ws=None):
+    """(dx, dA, dB): gradients of tb_packed_linear.  The adapters' (float, None without adapters) need xa from the forward pass
+    and its input, in full (x) or as `checkpoint`, the (codes, scales) of tb_checkpoint_pack."""
+    xt, wp, ap = _packed_call(w, adapters, dy, w.d_out, w.d_in)
+    n_tok, dev = dy.shape[0], dy.device
+    codes, cscales = checkpoint if checkpoint is not None else (None, None)
+    grads = adapters is not None and (x is not None or checkpoint is not None)
+    if grads:
+        if x is not None and (tuple(x.shape) != (n_tok, w.d_in) or x.dtype != dy.dtype):
+            raise ValueError("x must be [n_tok][d_in] of dy's dtype")
+        if codes is not None and (tuple(codes.shape) != (n_tok, w.d_in) or tuple(cscales.shape) != (n_tok, -(-w.d_in // 128))):
+            raise ValueError("checkpoint must be codes [n_tok][d_in] and scales [n_tok][d_in / 128]")
+        if xa is None or tuple(xa.shape) != (n_tok, adapters.rank):
+            raise ValueError("xa must be the forward pass's [n_tok][rank]")
+    dx = torch.empty((n_tok, w.d_in), dtype=dy.dtype, device=dev) if want_dx else None
+    dA = torch.empty(adapters.tensors[0].shape, dtype=torch.float32, device=dev) if grads else None
+    dB = torch.empty(adapters.tensors[1].shape, dtype=torch.float32, device=dev) if grads else None
+    _on_current(w, adapters, dy, x, codes, cscales, xa, ws)
+    lib = load()
+    if ws is None:
+        nbytes = lib.tb_packed_linear_backward_workspace(wp, ap, xt, n_tok)
+        ws = _workspace(nbytes, dev) if nbytes else None
+    _check(lib.tb_packed_linear_backward(wp, ap, _ptr(dy), xt, n_tok, _ptr(x, dy.dtype, True), _ptr(codes, torch.int8, True),
+                                         _ptr(cscales, torch.float32, True), _ptr(xa, torch.float32, True),
+                                         _ptr(dx, None, True), _ptr(dA, None, True), _ptr(dB, None, True),
+                                         _ptr(ws, None, True), 0 if ws is None else ws.numel(), _stream()),
+           "tb_packed_linear_backward")
+    return dx, dA, dB
+
+
+def tb_checkpoint_pack(x):
+    """x [n_tok][d] -> (codes int8 [n_tok][d], scales [n_tok][ceil(d / 128)]): activations in 8 bits."""
+    n_tok, d = x.shape
+    codes = torch.empty((n_tok, d), dtype=torch.int8, device=x.device)
+    scales = torch.empty((n_tok, -(-d // 128)), dtype=torch.float32, device=x.device)
+    if x.device.index != _current_device():
+        raise ValueError("tensors must live on the current device")
+    _check(load().tb_checkpoint_pack(_ptr(x), _xtype(x), n_tok, d, _ptr(codes), _ptr(scales), _stream()), "tb_checkpoint_pack")
+    return codes, scales
+
+
+def tb_checkpoint_unpack(codes, scales, dtype=torch.bfloat16):
+    """The values that tb_checkpoint_pack's codes and scales stand for."""
+    n_tok, d = codes.shape
+    if tuple(scales.shape) != (n_tok, -(-d // 128)):
+        raise ValueError("scales must be [n_tok][d / 128]")
+    x = torch.empty((n_tok, d), dtype=dtype, device=codes.device)
+    if _one_device((codes, scales)) != _current_device():
+        raise ValueError("tensors must live on the current device")
+    _check(load().tb_checkpoint_unpack(_ptr(codes, torch.int8), _ptr(scales, torch.float32), n_tok, d, _xtype(x), _ptr(x),
+                                       _stream()), "tb_checkpoint_unpack")
+    return x
 
 
 def tb_launch_count() -> int:

@@ -1,0 +1,171 @@
+// Activations kept in 8 bits: a scale max|x| / 127 for every token and run of 128 columns, codes rne(x / scale).
+//
+// Both kernels move data once and are bound by HBM.  Half a warp has a run: a lane holds 8 values (16 bytes of bf16, two
+// 16-byte loads of float), so a run's maximum is four shuffles away and a warp stores 256 bytes of codes.  A lane has two
+// such pieces in flight.
+//
+// The codes are those of the true quotient: x * (1 / scale) lands within one of it, and the sign of x - (q +- 1/2) scale,
+// which one fused multiply-add gives exactly, says whether q is the nearest; a tie (the sum is 0) goes to the even one.
+#include "tb_packed.cuh"
+
+namespace tb {
+
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
+  const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
+  const unsigned w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float4 q = __ldcs(reinterpret_cast<const float4*>(p) + h);
+    v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+  unsigned w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const unsigned*>(&b);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// rne(x / s) for finite x, |x| <= 127 s up to the rounding of s, s > 0; inv is about 1 / s
+__device__ __forceinline__ int nearest_code(float x, float s, float inv) {
+  float q = rintf(x * inv);
+  q = fminf(fmaxf(q, -127.0f), 127.0f);
+  const float up = fmaf(-(q + 0.5f), s, x), down = fmaf(-(q - 0.5f), s, x);
+  const bool odd = ((int)q) & 1;
+  if (up > 0.0f || (up == 0.0f && odd))
+    q += 1.0f;
+  else if (down < 0.0f || (down == 0.0f && odd))
+    q -= 1.0f;
+  return (int)fminf(fmaxf(q, -127.0f), 127.0f);
+}
+
+// Units of 8 values, numbered token by token with every token's last run filled up to 16 units.
+template <typename T>
+__global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x, signed char* __restrict__ codes,
+                                                         float* __restrict__ scales, long long n_runs, int d, int n_g) {
+  const int half = threadIdx.x >> 4, l = threadIdx.x & 15;
+  constexpr int PER = 2;
+  const long long r0 = (long long)blockIdx.x * (16 * PER) + half;
+  float v[PER][8];
+  bool in[PER];
+  long long at[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const long long run = r0 + 16 * k;
+    const long long t = run / n_g;
+    const int col = (int)(run - t * n_g) * CKPT_RUN + 8 * l;
+    in[k] = run < n_runs && col < d;
+    at[k] = t * d + col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
+    if (in[k]) load8(x + at[k], v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    unsigned top = 0;  // magnitudes as integers: they order like the values, and what is not finite comes out on top
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool finite = top < 0x7f800000u;
+    const float s = finite ? __fdiv_rn(__uint_as_float(top), 127.0f) : __uint_as_float(0x7fffffffu);
+    // a scale below 2^-126 has no float reciprocal worth the name: scaled up by 2^64 it has, and so has x
+    const bool tiny = s < 1.17549435e-38f;
+    const float up = tiny ? 18446744073709551616.0f : 1.0f;
+    const float su = s * up, inv = su > 0.0f ? 1.0f / su : 0.0f;
+    unsigned w[2] = {0, 0};
+    if (finite && su > 0.0f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const unsigned q = (unsigned)nearest_code(v[k][i] * up, su, inv) & 0xffu;
+        w[i >> 2] |= q << (8 * (i & 3));
+      }
+    }
+    if (in[k]) *reinterpret_cast<uint2*>(codes + at[k]) = make_uint2(w[0], w[1]);
+    if (l == 0 && r0 + 16 * k < n_runs) scales[r0 + 16 * k] = s;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_checkpoint_unpack(const signed char* __restrict__ codes,
+                                                           const float* __restrict__ scales, T* __restrict__ x,
+                                                           long long n_runs, int d, int n_g) {
+  const int half = threadIdx.x >> 4, l = threadIdx.x & 15;
+  constexpr int PER = 2;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const long long run = (long long)blockIdx.x * (16 * PER) + 16 * k + half;
+    const long long t = run / n_g;
+    const int col = (int)(run - t * n_g) * CKPT_RUN + 8 * l;
+    if (run >= n_runs || col >= d) continue;
+    const long long at = t * d + col;
+    const uint2 w = __ldcs(reinterpret_cast<const uint2*>(codes + at));
+    const float s = __ldg(scales + run);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(signed char)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
+    store8(x + at, v);
+  }
+}
+
+}  // namespace tb
+
+using namespace tb;
+
+static tb_status checkpoint_shape(tb_dtype type, long long n_tok, int d, const void* x, const void* codes,
+                                  const void* scales, long long* n_runs, unsigned* blocks) {
+  if ((type != TB_F32 && type != TB_BF16) || n_tok < 0 || d <= 0) return TB_ERR_INVALID_ARG;
+  if (d % 32) return TB_ERR_UNSUPPORTED;
+  *n_runs = n_tok * ((d + CKPT_RUN - 1) / CKPT_RUN);
+  const long long nb = (*n_runs + 31) / 32;
+  if (n_tok > 0x7fffffffll || nb > 0x7fffffffll) return TB_ERR_UNSUPPORTED;
+  *blocks = (unsigned)nb;
+  if (n_tok == 0) return TB_OK;
+  if (!x || !codes || !scales) return TB_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 4)) return TB_ERR_INVALID_ARG;
+  return TB_OK;
+}
+
+extern "C" tb_status tb_checkpoint_pack(const void* x, tb_dtype x_type, long long n_tok, int d, signed char* codes,
+                                        float* scales, void* stream) {
+  long long n_runs;
+  unsigned nb;
+  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb));
+  if (nb == 0) return TB_OK;
+  const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
+  if (x_type == TB_BF16)
+    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const __nv_bfloat16*>(x), codes, scales, n_runs, d, n_g);
+  else
+    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const float*>(x), codes, scales, n_runs, d, n_g);
+  TB_LAUNCH_CHECK();
+  return TB_OK;
+}
+
+extern "C" tb_status tb_checkpoint_unpack(const signed char* codes, const float* scales, long long n_tok, int d,
+                                          tb_dtype x_type, void* x, void* stream) {
+  long long n_runs;
+  unsigned nb;
+  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb));
+  if (nb == 0) return TB_OK;
+  const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
+  if (x_type == TB_BF16)
+    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<__nv_bfloat16*>(x), n_runs, d, n_g);
+  else
+    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<float*>(x), n_runs, d, n_g);
+  TB_LAUNCH_CHECK();
+  return TB_OK;
+}

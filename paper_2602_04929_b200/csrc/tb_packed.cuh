@@ -1,0 +1,56 @@
+// Shared pieces of the products with bit-packed weights (tb_packed_linear and its gradients).
+#pragma once
+
+#include "tb_common.cuh"
+
+namespace tb {
+
+// A packed projection and the adapters beside it as the kernels take them.
+struct PackedW {
+  const unsigned int* packed;
+  const float* scales;
+  const int* zeros;
+  int d_out, d_in, bits, group, n_g, words;  // group: columns of a scale (d_in where there is one a row); words of a row
+};
+struct Adapt {  // n = 0: none
+  const void *A, *B;
+  const float* scale;
+  const int *starts, *ids;
+  int n, rank, n_req;
+};
+
+// The adapter of token t, or -1: the last request that starts at or before t, if t is not behind all of them.  Whatever
+// the device arrays hold, the search ends and the result indexes an adapter or nothing.
+__device__ __forceinline__ int adapter_of(const Adapt& a, long long t) {
+  int lo = -1, hi = a.n_req;  // starts[lo] <= t < starts[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a.starts[mid] <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  if (lo < 0 || a.starts[a.n_req] <= t) return -1;
+  const int id = a.ids[lo];
+  return id >= 0 && id < a.n ? id : -1;
+}
+
+// N codes from code j of a row on (j a multiple of 8, so the codes start on a byte), `row` its first word.
+template <int N>
+__device__ __forceinline__ void unpack_codes(const unsigned int* row, int words, int j, int bits, unsigned (&c)[N]) {
+  const unsigned mask = (1u << bits) - 1u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int pos = (j + i) * bits, w = pos >> 5, s = pos & 31;
+    unsigned v = row[w] >> s;
+    if (s + bits > 32) v |= row[w + 1] << (32 - s);  // a code never crosses the end of its row
+    c[i] = v & mask;
+  }
+}
+
+// The input of a product of gradients: in full, or 8-bit codes with a scale for a token and CKPT_RUN columns.
+constexpr int CKPT_RUN = 128;
+
+int sm_count();  // of the current device, 0 where it cannot be asked
+
+}  // namespace tb

@@ -1,0 +1,130 @@
+// Products with bit-packed weights, low-rank adapters of many requests beside them, and their gradients: the entry points.
+#include "tb_packed.cuh"
+
+namespace tb {
+
+int sm_count() {
+  static int count[64] = {0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  if (!count[dev]) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    count[dev] = n;
+  }
+  return count[dev];
+}
+
+tb_status packed_product_simt(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out,
+                              const float* low, bool back, cudaStream_t st);
+tb_status adapter_low_simt(const Adapt& ad, const void* in, const void* M, tb_dtype type, long long n_tok, int width, float* low,
+                           cudaStream_t st);
+tb_status adapter_grad_simt(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low,
+                            long long n_tok, int width, float* G, cudaStream_t st);
+
+// Shapes first (so that the workspace queries can use them), pointers with `with_data`.
+static tb_status checked(const tb_packed_weight* w, const tb_adapters* a, tb_dtype type, long long n_tok, bool with_data,
+                         PackedW* pw, Adapt* ad) {
+  if (!w || (type != TB_F32 && type != TB_BF16) || n_tok < 0) return TB_ERR_INVALID_ARG;
+  if (w->d_out <= 0 || w->d_in <= 0 || w->bits < 2 || w->bits > 8 || w->quant_group < 0) return TB_ERR_INVALID_ARG;
+  if (w->quant_group > 0 && w->d_in % w->quant_group) return TB_ERR_INVALID_ARG;
+  if (a && (a->n_adapters < 1 || a->rank < 1 || a->n_requests < 1)) return TB_ERR_INVALID_ARG;
+  if (w->d_in % 32 || w->d_out % 8 || w->quant_group % 32) return TB_ERR_UNSUPPORTED;
+  if (n_tok > 0x7fffffffll / 2 || w->d_out > (1 << 24) || w->d_in > (1 << 24)) return TB_ERR_UNSUPPORTED;
+  if (a && (a->rank % 8 || a->rank > 128 || a->n_adapters > 65535)) return TB_ERR_UNSUPPORTED;
+  if (with_data) {
+    if (!w->packed || !w->scales || !w->zeros) return TB_ERR_INVALID_ARG;
+    if (!aligned(w->packed, 16) || !aligned(w->scales, 4) || !aligned(w->zeros, 4)) return TB_ERR_INVALID_ARG;
+    if (a && (!a->A || !a->B || !a->scale || !a->starts || !a->ids)) return TB_ERR_INVALID_ARG;
+    if (a && (!aligned(a->A, 16) || !aligned(a->B, 16) || !aligned(a->scale, 4) || !aligned(a->starts, 4) || !aligned(a->ids, 4)))
+      return TB_ERR_INVALID_ARG;
+  }
+  pw->packed = w->packed, pw->scales = w->scales, pw->zeros = w->zeros;
+  pw->d_out = w->d_out, pw->d_in = w->d_in, pw->bits = w->bits;
+  pw->group = w->quant_group ? w->quant_group : w->d_in;
+  pw->n_g = w->d_in / pw->group;
+  pw->words = w->d_in / 32 * w->bits;
+  *ad = Adapt{};
+  if (a) {
+    ad->A = a->A, ad->B = a->B, ad->scale = a->scale, ad->starts = a->starts, ad->ids = a->ids;
+    ad->n = a->n_adapters, ad->rank = a->rank, ad->n_req = a->n_requests;
+  }
+  return TB_OK;
+}
+
+// Scratch of the backward pass: u = dy B^T of every token, not scaled.
+static size_t carve_backward(const Adapt& ad, long long n_tok, char* ws, float** u) {
+  Bump b(ws);
+  *u = ad.n ? b.take<float>((size_t)n_tok * ad.rank) : nullptr;
+  return ad.n ? b.total() : 0;
+}
+
+}  // namespace tb
+
+using namespace tb;
+
+extern "C" size_t tb_packed_linear_workspace(const tb_packed_weight* w, const tb_adapters* adapters, tb_dtype x_type,
+                                             long long n_tok) {
+  PackedW pw;
+  Adapt ad;
+  if (checked(w, adapters, x_type, n_tok, false, &pw, &ad) != TB_OK || n_tok == 0) return 0;
+  return 0;
+}
+
+extern "C" tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapters, const void* x, tb_dtype x_type,
+                                      long long n_tok, void* y, float* xa, void* ws, size_t ws_bytes, void* stream) {
+  PackedW pw;
+  Adapt ad;
+  TB_TRY(checked(w, adapters, x_type, n_tok, true, &pw, &ad));
+  if (n_tok == 0) return TB_OK;
+  if (!x || !y || (ad.n && !xa)) return TB_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(xa, 16)) return TB_ERR_INVALID_ARG;
+  const size_t need = tb_packed_linear_workspace(w, adapters, x_type, n_tok);
+  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return TB_ERR_WORKSPACE;
+  cudaStream_t st = as_stream(stream);
+  if (ad.n) TB_TRY(adapter_low_simt(ad, x, ad.A, x_type, n_tok, pw.d_in, xa, st));
+  return packed_product_simt(pw, ad, x, x_type, n_tok, y, xa, false, st);
+}
+
+extern "C" size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters, tb_dtype x_type,
+                                                      long long n_tok) {
+  PackedW pw;
+  Adapt ad;
+  float* u;
+  if (checked(w, adapters, x_type, n_tok, false, &pw, &ad) != TB_OK || n_tok == 0) return 0;
+  return carve_backward(ad, n_tok, nullptr, &u);
+}
+
+extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const tb_adapters* adapters, const void* dy,
+                                               tb_dtype x_type, long long n_tok, const void* x, const signed char* x_codes,
+                                               const float* x_scales, const float* xa, void* dx, float* dA, float* dB, void* ws,
+                                               size_t ws_bytes, void* stream) {
+  PackedW pw;
+  Adapt ad;
+  TB_TRY(checked(w, adapters, x_type, n_tok, true, &pw, &ad));
+  if ((dA == nullptr) != (dB == nullptr) || (dA && !ad.n) || (!dx && !dA)) return TB_ERR_INVALID_ARG;
+  if (!aligned(dA, 16) || !aligned(dB, 16)) return TB_ERR_INVALID_ARG;
+  cudaStream_t st = as_stream(stream);
+  if (n_tok == 0) {
+    if (dA) {
+      TB_CUDA_CHECK(cudaMemsetAsync(dA, 0, (size_t)ad.n * ad.rank * pw.d_in * sizeof(float), st));
+      TB_CUDA_CHECK(cudaMemsetAsync(dB, 0, (size_t)ad.n * ad.rank * pw.d_out * sizeof(float), st));
+    }
+    return TB_OK;
+  }
+  if (!dy || !aligned(dy, 16) || !aligned(dx, 16)) return TB_ERR_INVALID_ARG;
+  if (dA) {  // the input in one of its two forms
+    if (!xa || (x != nullptr) == (x_codes != nullptr) || (x_codes != nullptr) != (x_scales != nullptr)) return TB_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(x_codes, 16) || !aligned(x_scales, 4) || !aligned(xa, 16)) return TB_ERR_INVALID_ARG;
+  }
+  float* u;
+  const size_t need = carve_backward(ad, n_tok, static_cast<char*>(ws), &u);
+  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return TB_ERR_WORKSPACE;
+  if (ad.n) TB_TRY(adapter_low_simt(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
+  if (dx) TB_TRY(packed_product_simt(pw, ad, dy, x_type, n_tok, dx, u, true, st));
+  if (dA) {
+    TB_TRY(adapter_grad_simt(ad, x_codes ? (const void*)x_codes : x, x_scales, x_type, u, n_tok, pw.d_in, dA, st));
+    TB_TRY(adapter_grad_simt(ad, dy, nullptr, x_type, xa, n_tok, pw.d_out, dB, st));
+  }
+  return TB_OK;
+}

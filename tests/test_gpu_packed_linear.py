@@ -1,0 +1,319 @@
+"""Products with bit-packed weights, adapters beside them and their gradients, element by element against double precision."""
+import pytest
+import torch
+
+import packed_util as pu
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _tb():
+    import paper_2602_04929_b200 as tb
+    return tb
+
+
+def _forward(p, what=""):
+    tb = _tb()
+    w, a = pu.on_gpu(tb, p)
+    y, xa = tb.tb_packed_linear(w, p["x"].cuda(), a)
+    want, xa64, bound = pu.forward64(p)
+    pu.near(y, want, bound, what)
+    assert pu.norm_off(y, want) <= pu.HALF_STEP[p["dtype"]] + 1e-6
+    if a is None:
+        assert xa is None
+    else:
+        pu.near(xa, xa64, (p["d"] + 64) * 2.0 ** -23 * (p["x"].double().abs().amax(1, keepdim=True) * p["d"]), what)
+        assert pu.norm_off(xa, xa64) <= 2e-6
+        assert not xa[(pu.owners(p) < 0).cuda()].any()
+    assert tb.tb_device_error_flag() == 0
+    return y, xa
+
+
+@pytest.mark.parametrize("bits", range(2, 9))
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n_tok", [1, 5, 19, 130])
+def test_every_width_of_code(bits, dtype, n_tok):
+    _forward(pu.problem(bits, n_tok, 152, 384, bits, 128, dtype))
+
+
+@pytest.mark.parametrize("rows,d,group", [(8, 32, 0), (24, 32, 32), (136, 96, 96), (264, 160, 32), (128, 544, 0), (1032, 128, 64),
+                                          (256, 1024, 256), (520, 1152, 384), (16, 2080, 416), (2056, 640, 128)])
+@pytest.mark.parametrize("n_tok", [1, 2, 8, 9, 16, 17, 33, 64, 65, 129, 256, 257])
+def test_shapes(rows, d, group, n_tok):
+    _forward(pu.problem(rows + d, n_tok, rows, d, 3 if rows % 16 else 4, group, BF), (rows, d, group, n_tok))
+
+
+@pytest.mark.parametrize("rows,d,group", [(24, 32, 0), (264, 160, 32), (520, 1152, 384)])
+@pytest.mark.parametrize("n_tok", [1, 9, 70, 300])
+def test_shapes_float(rows, d, group, n_tok):
+    _forward(pu.problem(rows + d, n_tok, rows, d, 2, group, F32), (rows, d, group, n_tok))
+
+
+REQUESTS = {
+    "one": (40, [0, 40], [0]),
+    "single tokens": (11, list(range(12)), [3, 1, 1, -1, 0, 2, 3, 9, 0, 0, 1]),
+    "empty ones": (37, [0, 0, 5, 5, 5, 30, 37, 37], [1, 0, 2, 3, 2, 1, 0]),
+    "none": (20, [0, 10, 20], [-1, 4]),
+    "gaps at both ends": (50, [7, 9, 31], [2, 0]),
+    "ragged": (301, [0, 1, 18, 19, 140, 290, 301], [3, 0, 1, 2, 0, 3]),
+    "long": (600, [0, 250, 600], [1, 1]),
+}
+
+
+def _with_adapters(name, rank, dtype, rows=264, d=416, bits=4, group=32):
+    n_tok, starts, ids = REQUESTS[name]
+    return pu.problem(len(name) + rank, n_tok, rows, d, bits, group, dtype, 4, rank, starts, ids)
+
+
+@pytest.mark.parametrize("name", REQUESTS)
+@pytest.mark.parametrize("rank", [8, 16, 40, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_adapters(name, rank, dtype):
+    _forward(_with_adapters(name, rank, dtype), name)
+
+
+@pytest.mark.parametrize("name", REQUESTS)
+@pytest.mark.parametrize("rank,dtype", [(8, BF), (40, BF), (128, BF), (16, F32)])
+@pytest.mark.parametrize("kept", ["full", "8 bits"])
+def test_gradients(name, rank, dtype, kept):
+    tb = _tb()
+    p = _with_adapters(name, rank, dtype)
+    w, a = pu.on_gpu(tb, p)
+    xa = pu.forward64(p)[1].float()
+    if kept == "full":
+        x, how = None, dict(x=p["x"].cuda())
+    else:
+        codes, scales = pu.eight_bits(p["x"])
+        x = torch.from_numpy(codes).double() * torch.from_numpy(scales).double().repeat_interleave(128, 1)[:, :p["d"]]
+        how = dict(checkpoint=(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()))
+    out = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, xa=xa.cuda(), **how)
+    for name_, got in zip(("dx", "dA", "dB"), out):
+        want, bound = pu.backward64(p, x, xa)[name_]
+        pu.near(got, want, bound, (name, name_))
+        if name_ != "dx" and want.any():
+            assert pu.norm_off(got, want) <= 3e-6, name_
+    again = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, xa=xa.cuda(), **how)
+    assert all(torch.equal(g, h) for g, h in zip(out, again))
+    assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("rows,d,group,bits", [(8, 32, 0, 2), (136, 96, 96, 3), (264, 160, 32, 5), (1032, 544, 0, 7), (256, 1024, 128, 8),
+                                               (520, 1152, 384, 6)])
+@pytest.mark.parametrize("n_tok", [1, 16, 33, 129, 260])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_input_gradient_alone(rows, d, group, bits, n_tok, dtype):
+    tb = _tb()
+    p = pu.problem(rows, n_tok, rows, d, bits, group, dtype)
+    w, _ = pu.on_gpu(tb, p)
+    dx, dA, dB = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    assert dA is None and dB is None
+    want, bound = pu.backward64(p)["dx"]
+    pu.near(dx, want, bound)
+    assert pu.norm_off(dx, want) <= (1.5 * pu.HALF_STEP[dtype] if dtype == BF else 2e-6)
+
+
+def test_gradients_against_differences():
+    """dx, dA and dB are the slopes of sum(y * g): the function is linear in x and in each adapter matrix, so a difference of any
+    step is exact up to rounding (float, steps of the values' own size)."""
+    tb = _tb()
+    p = pu.problem(3, 29, 40, 64, 4, 32, F32, 2, 8, [0, 11, 29], [1, 0])
+    g = p["dy"].double()
+
+    def value(q):
+        w, a = pu.on_gpu(tb, q)
+        return (tb.tb_packed_linear(w, q["x"].cuda(), a)[0].cpu().double() * g).sum()
+
+    w, a = pu.on_gpu(tb, p)
+    y, xa = tb.tb_packed_linear(w, p["x"].cuda(), a)
+    grads = dict(zip(("x", "A", "B"), tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, x=p["x"].cuda(), xa=xa)))
+    r = torch.Generator().manual_seed(5)
+    for name, grad in grads.items():
+        step = torch.randn(p[name].shape, generator=r)
+        up, down = dict(p), dict(p)
+        up[name], down[name] = p[name] + step, p[name] - step
+        slope = (value(up) - value(down)) / 2
+        want = (grad.cpu().double() * step.double()).sum()
+        # 29 x 40 outputs of sums of 64 + 8 products, a few units in magnitude, each in float
+        assert abs(slope - want) <= 1e-5 * (g.abs().sum() + abs(want)), name
+
+
+def test_a_run_of_them_as_in_training():
+    """Forward, the input kept in 8 bits, backward from it: the adapters' gradients are those of the decoded input."""
+    tb = _tb()
+    n_tok, starts, ids = REQUESTS["ragged"]
+    p = pu.problem(9, n_tok, 392, 640, 2, 128, BF, 4, 16, starts, ids)
+    w, a = pu.on_gpu(tb, p)
+    x = p["x"].cuda()
+    y, xa = tb.tb_packed_linear(w, x, a)
+    kept = tb.tb_checkpoint_pack(x)
+    del x
+    dx, dA, dB = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, checkpoint=kept, xa=xa)
+    x8 = tb.tb_checkpoint_unpack(*kept, dtype=F32).cpu()
+    assert (x8.double() - p["x"].double()).abs().max() <= 0.5 * kept[1].max().item() * 1.0001
+    want = pu.backward64(p, x8, xa.cpu())
+    for name, got in (("dx", dx), ("dA", dA), ("dB", dB)):
+        pu.near(got, *want[name], name)
+    yw, _, bound = pu.forward64(p)
+    pu.near(y, yw, bound)
+
+
+def test_quantized_layer_to_product():
+    """From the quantizer's own outputs: codes packed, the product is that with the dequantized weights."""
+    import numpy as np
+    import parity_util as qu
+    tb = _tb()
+    prob = qu.make_problem(1, 256, 2, 32, 1024, with_r=False)
+    res = qu.run_gpu(prob, 3, 128, 8, 3)
+    t = lambda v: torch.from_numpy(np.ascontiguousarray(v))  # noqa: E731
+    packed = tb.tb_pack_codes(t(res["codes"]).cuda(), 3)
+    w = tb.packed_weight(packed, t(res["scales"]).cuda(), t(res["zeros"]).cuda(), 256, 3, 128)
+    x = torch.randn((21, 256), generator=torch.Generator().manual_seed(2)).to(BF)
+    y, _ = tb.tb_packed_linear(w, x.cuda())
+    Q = t(res["scales"]).double().repeat_interleave(128, 1) * (t(res["codes"]).double() - t(res["zeros"]).double().repeat_interleave(128, 1))
+    want = x.double() @ Q.T
+    pu.near(y, want, pu.HALF_STEP[BF] * want.abs() + pu.sum_bound(256, x.double().abs() @ Q.abs().T, BF))
+
+
+@pytest.mark.parametrize("n_tok,starts", [(24, [0, 3, 9, 24]), (200, [0, 50, 133, 200])])
+@pytest.mark.parametrize("rank", [8, 64])
+def test_what_is_not_finite_stays_with_its_own(n_tok, starts, rank):
+    """An infinite or undefined activation changes its own token alone, and one in an adapter its requests alone."""
+    tb = _tb()
+    ids = [1, 0, 1]
+    p = pu.problem(4, n_tok, 264, 256, 4, 128, BF, 3, rank, starts, ids)
+    p["x"][starts[1] + 2, 17] = float("inf")
+    p["x"][starts[1] + 4, 200] = float("nan")
+    p["A"][2] = float("nan")                       # no request has this one
+    clean = dict(p, A=p["A"].clone(), B=p["B"].clone(), x=p["x"].clone())
+    clean["x"][starts[1] + 2, 17], clean["x"][starts[1] + 4, 200] = 0.0, 0.0
+    p["B"][0, 3, 100] = float("inf")
+    w, a = pu.on_gpu(tb, p)
+    y, xa = (v.cpu() for v in tb.tb_packed_linear(w, p["x"].cuda(), a))
+    want, xa64, bound = pu.forward64(clean)
+    hit = torch.zeros(n_tok, dtype=torch.bool)
+    hit[[starts[1] + 2, starts[1] + 4]] = True
+    own0 = pu.owners(p) == 0
+    fine = ~hit
+    assert ((y[fine].double() - want[fine]).abs() <= bound[fine])[:, :100].all()
+    assert ((y[fine].double() - want[fine]).abs() <= bound[fine])[:, 101:].all()
+    assert torch.isfinite(y[fine & ~own0]).all() and not torch.isfinite(y[own0][:, 100]).any()
+    # 0 is among the values of c - z, so an infinite activation gives what is no number or an infinity in every column
+    assert not torch.isfinite(y[hit]).any() and not torch.isfinite(xa[hit]).any() and torch.isfinite(xa[fine]).all()
+    # backward: an undefined token of one adapter leaves the other adapters' gradients alone
+    q = dict(clean, dy=p["dy"].clone())
+    q["dy"][starts[1] + 2, 5] = float("nan")
+    w, a = pu.on_gpu(tb, q)
+    x = q["x"].clone()
+    x[starts[1] + 3, 9] = float("inf")
+    dx, dA, dB = tb.tb_packed_linear_backward(w, q["dy"].cuda(), a, x=x.cuda(), xa=xa64.float().cuda())
+    ref = pu.backward64(q, None, xa64.float())
+    for got, name in ((dA, "dA"), (dB, "dB")):
+        pu.near(got[1], ref[name][0][1], ref[name][1][1], name)
+        assert not got[2].any()
+        assert torch.isnan(got[0]).any()
+    rows = torch.ones(n_tok, dtype=torch.bool)
+    rows[starts[1] + 2] = False
+    pu.near(dx[rows.cuda()], ref["dx"][0][rows], ref["dx"][1][rows], "dx")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_no_tokens(dtype):
+    tb = _tb()
+    p = pu.problem(1, 0, 64, 96, 3, 32, dtype, 2, 8, [0, 0], [1])
+    w, a = pu.on_gpu(tb, p)
+    y, xa = tb.tb_packed_linear(w, p["x"].cuda(), a)
+    assert y.shape == (0, 64) and xa.shape == (0, 8)
+    dx, dA, dB = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, x=p["x"].cuda(), xa=xa)
+    assert dx.shape == (0, 96) and not dA.any() and not dB.any()
+    codes, scales = tb.tb_checkpoint_pack(p["x"].cuda())
+    assert tb.tb_checkpoint_unpack(codes, scales).shape == (0, 96)
+
+
+@pytest.mark.parametrize("n_tok", [3, 40, 333])
+def test_captured_and_on_another_stream(n_tok):
+    """Two captured graphs and eager calls between their replays: each sees its own inputs, bits as from an eager call."""
+    tb = _tb()
+    starts, ids = [0, n_tok // 2, n_tok], [1, 0]
+    probs = [pu.problem(s, n_tok, 264, 512, 2, 128, BF, 2, 16, starts, ids) for s in (1, 2)]
+    want, graphs, outs, ins = [], [], [], []
+    for p in probs:
+        w, a = pu.on_gpu(tb, p)
+        x, dy = p["x"].cuda(), p["dy"].cuda()
+
+        def call(w=w, a=a, x=x, dy=dy):
+            y, xa = tb.tb_packed_linear(w, x, a)
+            kept = tb.tb_checkpoint_pack(x)
+            return (y, xa) + tb.tb_packed_linear_backward(w, dy, a, checkpoint=kept, xa=xa)
+
+        want.append(call())
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = call()
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(u, v) for u, v in zip(other, want[-1]))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call())
+        graphs.append(g)
+        ins.append((x, dy, w, a))   # a graph holds addresses: what it reads has to live on
+    for k in (0, 1, 1, 0):
+        for t in outs[k]:
+            t.zero_()
+        graphs[k].replay()
+        tb.tb_packed_linear(w, x, a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(outs[k], want[k]))
+    ins[0][0].copy_(ins[1][0])                      # new inputs in the captured buffers
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    w, a = pu.on_gpu(tb, probs[0])
+    assert torch.equal(outs[0][0], tb.tb_packed_linear(w, ins[1][0], a)[0])
+
+
+def test_neighbours_of_the_outputs_stay():
+    """Guard values before and behind every output."""
+    tb = _tb()
+    for n_tok in (3, 21, 150):
+        p = pu.problem(n_tok, n_tok, 136, 160, 3, 32, BF, 1, 8, [0, n_tok], [0])
+        w, a = pu.on_gpu(tb, p)
+        buf = torch.full((n_tok * 136 + 128,), 7.0, dtype=BF, device="cuda")
+        low = torch.full((n_tok * 8 + 128,), 7.0, device="cuda")
+        y, xa = buf[64:64 + n_tok * 136].view(n_tok, 136), low[64:64 + n_tok * 8].view(n_tok, 8)
+        tb.tb_packed_linear(w, p["x"].cuda(), a, y=y, xa=xa)
+        want, xa64, bound = pu.forward64(p)
+        pu.near(y, want, bound)
+        for b, n in ((buf, n_tok * 136), (low, n_tok * 8)):
+            assert (b[:64] == 7).all() and (b[64 + n:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n_tok,d", [(1, 32), (3, 96), (5, 128), (17, 160), (33, 4096), (257, 1184)])
+def test_8_bit_form(n_tok, d, dtype):
+    tb = _tb()
+    x = pu.problem(n_tok, n_tok, 8, d, 2, 0, dtype)["x"]
+    if n_tok > 2:
+        x[1] = 0.0
+        x[2] *= 1e-38
+        x[0, :min(d, 128)] = torch.arange(min(d, 128)) * 0.5      # ties: the quotients are halves where the scale is 1
+        x[0, 0] = 127.0
+    codes, scales = tb.tb_checkpoint_pack(x.cuda())
+    cw, sw = pu.eight_bits(x)
+    assert (scales.cpu().numpy() == sw).all() and (codes.cpu().numpy() == cw).all()
+    got = tb.tb_checkpoint_unpack(codes, scales, dtype)
+    want = (torch.from_numpy(cw).float() * torch.from_numpy(sw).repeat_interleave(128, 1)[:, :d]).to(dtype)
+    assert torch.equal(got.cpu(), want)
+
+
+def test_8_bit_form_of_what_is_not_finite():
+    tb = _tb()
+    x = torch.ones((4, 288), dtype=BF)
+    x[0, 130], x[1, 0], x[2, 287] = float("inf"), float("nan"), float("-inf")
+    codes, scales = tb.tb_checkpoint_pack(x.cuda())
+    v = tb.tb_checkpoint_unpack(codes, scales, F32).cpu()
+    bad = torch.zeros((4, 3), dtype=torch.bool)
+    bad[0, 1] = bad[1, 0] = bad[2, 2] = True
+    assert torch.equal(torch.isnan(scales).cpu(), bad)
+    assert torch.equal(torch.isnan(v), bad.repeat_interleave(128, 1)[:, :288])
+    assert ((v[3] - 1).abs() < 1e-6).all()
