@@ -1,5 +1,5 @@
 // Products with bit-packed weights, low-rank adapters of many requests beside them, and their gradients: the entry points.
-#include "tb_packed.cuh"
+#include "tb_packed_plan.cuh"
 
 namespace tb {
 
@@ -52,11 +52,32 @@ static tb_status checked(const tb_packed_weight* w, const tb_adapters* a, tb_dty
   return TB_OK;
 }
 
-// Scratch of the backward pass: u = dy B^T of every token, not scaled.
-static size_t carve_backward(const Adapt& ad, long long n_tok, char* ws, float** u) {
+// Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.
+struct Scratch {
+  float* u;
+  char* product;
+  size_t bytes;
+};
+static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long n_tok, bool back, void* ws) {
+  Scratch s;
   Bump b(ws);
-  *u = ad.n ? b.take<float>((size_t)n_tok * ad.rank) : nullptr;
-  return ad.n ? b.total() : 0;
+  s.u = back && ad.n ? b.take<float>((size_t)n_tok * ad.rank) : nullptr;
+  size_t n = 0;
+  if (type == TB_BF16) {
+    PackedTc p;
+    const int cols = back ? w.d_in : w.d_out;
+    n = packed_tc_carve(packed_tc_plan((int)n_tok, cols, back ? w.d_out : w.d_in), ad, (int)n_tok, cols, nullptr, &p);
+  }
+  s.product = b.take<char>(n);
+  s.bytes = (back && ad.n) || n ? b.total() : 0;
+  return s;
+}
+
+static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out, const float* low,
+                         bool back, void* ws, cudaStream_t st) {
+  if (type == TB_BF16)
+    return packed_product_tc(w, ad, static_cast<const __nv_bfloat16*>(in), n_tok, static_cast<__nv_bfloat16*>(out), low, back, ws, st);
+  return packed_product_simt(w, ad, in, type, n_tok, out, low, back, st);
 }
 
 }  // namespace tb
@@ -68,7 +89,7 @@ extern "C" size_t tb_packed_linear_workspace(const tb_packed_weight* w, const tb
   PackedW pw;
   Adapt ad;
   if (checked(w, adapters, x_type, n_tok, false, &pw, &ad) != TB_OK || n_tok == 0) return 0;
-  return 0;
+  return carve(pw, ad, x_type, n_tok, false, nullptr).bytes;
 }
 
 extern "C" tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapters, const void* x, tb_dtype x_type,
@@ -79,20 +100,19 @@ extern "C" tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapte
   if (n_tok == 0) return TB_OK;
   if (!x || !y || (ad.n && !xa)) return TB_ERR_INVALID_ARG;
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(xa, 16)) return TB_ERR_INVALID_ARG;
-  const size_t need = tb_packed_linear_workspace(w, adapters, x_type, n_tok);
-  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return TB_ERR_WORKSPACE;
+  const Scratch sc = carve(pw, ad, x_type, n_tok, false, ws);
+  if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
   cudaStream_t st = as_stream(stream);
   if (ad.n) TB_TRY(adapter_low_simt(ad, x, ad.A, x_type, n_tok, pw.d_in, xa, st));
-  return packed_product_simt(pw, ad, x, x_type, n_tok, y, xa, false, st);
+  return product(pw, ad, x, x_type, n_tok, y, xa, false, sc.product, st);
 }
 
 extern "C" size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters, tb_dtype x_type,
                                                       long long n_tok) {
   PackedW pw;
   Adapt ad;
-  float* u;
   if (checked(w, adapters, x_type, n_tok, false, &pw, &ad) != TB_OK || n_tok == 0) return 0;
-  return carve_backward(ad, n_tok, nullptr, &u);
+  return carve(pw, ad, x_type, n_tok, true, nullptr).bytes;
 }
 
 extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const tb_adapters* adapters, const void* dy,
@@ -117,11 +137,11 @@ extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const 
     if (!xa || (x != nullptr) == (x_codes != nullptr) || (x_codes != nullptr) != (x_scales != nullptr)) return TB_ERR_INVALID_ARG;
     if (!aligned(x, 16) || !aligned(x_codes, 16) || !aligned(x_scales, 4) || !aligned(xa, 16)) return TB_ERR_INVALID_ARG;
   }
-  float* u;
-  const size_t need = carve_backward(ad, n_tok, static_cast<char*>(ws), &u);
-  if (need && (!ws || !aligned(ws, 256) || ws_bytes < need)) return TB_ERR_WORKSPACE;
+  const Scratch sc = carve(pw, ad, x_type, n_tok, true, ws);
+  if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
+  float* u = sc.u;
   if (ad.n) TB_TRY(adapter_low_simt(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
-  if (dx) TB_TRY(packed_product_simt(pw, ad, dy, x_type, n_tok, dx, u, true, st));
+  if (dx) TB_TRY(product(pw, ad, dy, x_type, n_tok, dx, u, true, sc.product, st));
   if (dA) {
     TB_TRY(adapter_grad_simt(ad, x_codes ? (const void*)x_codes : x, x_scales, x_type, u, n_tok, pw.d_in, dA, st));
     TB_TRY(adapter_grad_simt(ad, dy, nullptr, x_type, xa, n_tok, pw.d_out, dB, st));

@@ -254,6 +254,8 @@ int grid_digits_error_read_clear();  // the grid search's products (tb_grid_digi
 int sweep_error_read_clear();  // the same word of the column-sweep kernel (tb_sweep.cu)
 int yw_error_read_clear();     // and of the tensor-core product of the scale refinement (tb_gemm_tc.cu)
 int cross_error_read_clear();  // and of the deviation correlation (tb_cross_tc.cu)
+int packed_fwd_error_read_clear();  // the products with bit-packed weights (tb_packed_tc_fwd.cu,
+int packed_bwd_error_read_clear();  // tb_packed_tc_bwd.cu)
 int pair_error_read_clear();   // and of the CTA-pair form of the Hessian kernel (tb_syrk_tc2.cu)
 }
 
@@ -297,6 +299,8 @@ extern "C" int tb_device_error_flag(void) {
   const int y = tb::yw_error_read_clear();
   const int x = tb::cross_error_read_clear();
   const int q = tb::pair_error_read_clear();
-  if (e < 0 || c < 0 || g < 0 || w < 0 || y < 0 || x < 0 || q < 0) return -1;
-  return (v || e || c || g || w || y || x || q) ? 1 : 0;
+  const int pf = tb::packed_fwd_error_read_clear();
+  const int pb = tb::packed_bwd_error_read_clear();
+  if (e < 0 || c < 0 || g < 0 || w < 0 || y < 0 || x < 0 || q < 0 || pf < 0 || pb < 0) return -1;
+  return (v || e || c || g || w || y || x || q || pf || pb) ? 1 : 0;
 }
