@@ -22,6 +22,24 @@ tb_status adapter_low_simt(const Adapt& ad, const void* in, const void* M, tb_dt
 tb_status adapter_grad_simt(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low,
                             long long n_tok, int width, float* G, cudaStream_t st);
 
+tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
+                           cudaStream_t st);
+tb_status adapter_grad_bf16(const Adapt& ad, const void* in, const float* in_scales, const float* low, int n_tok, int width, float* G,
+                            cudaStream_t st);
+
+static tb_status adapter_low(const Adapt& ad, const void* in, const void* M, tb_dtype type, long long n_tok, int width, float* low,
+                             cudaStream_t st) {
+  if (type == TB_BF16)
+    return adapter_low_bf16(ad, static_cast<const __nv_bfloat16*>(in), static_cast<const __nv_bfloat16*>(M), (int)n_tok, width, low, st);
+  return adapter_low_simt(ad, in, M, type, n_tok, width, low, st);
+}
+// of an input in `type`, or of 8-bit codes where their scales are given
+static tb_status adapter_grad(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low, long long n_tok,
+                              int width, float* G, cudaStream_t st) {
+  if (type == TB_BF16) return adapter_grad_bf16(ad, in, in_scales, low, (int)n_tok, width, G, st);
+  return adapter_grad_simt(ad, in, in_scales, type, low, n_tok, width, G, st);
+}
+
 // Shapes first (so that the workspace queries can use them), pointers with `with_data`.
 static tb_status checked(const tb_packed_weight* w, const tb_adapters* a, tb_dtype type, long long n_tok, bool with_data,
                          PackedW* pw, Adapt* ad) {
@@ -103,7 +121,7 @@ extern "C" tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapte
   const Scratch sc = carve(pw, ad, x_type, n_tok, false, ws);
   if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
   cudaStream_t st = as_stream(stream);
-  if (ad.n) TB_TRY(adapter_low_simt(ad, x, ad.A, x_type, n_tok, pw.d_in, xa, st));
+  if (ad.n) TB_TRY(adapter_low(ad, x, ad.A, x_type, n_tok, pw.d_in, xa, st));
   return product(pw, ad, x, x_type, n_tok, y, xa, false, sc.product, st);
 }
 
@@ -140,11 +158,11 @@ extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const 
   const Scratch sc = carve(pw, ad, x_type, n_tok, true, ws);
   if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
   float* u = sc.u;
-  if (ad.n) TB_TRY(adapter_low_simt(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
+  if (ad.n) TB_TRY(adapter_low(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
   if (dx) TB_TRY(product(pw, ad, dy, x_type, n_tok, dx, u, true, sc.product, st));
   if (dA) {
-    TB_TRY(adapter_grad_simt(ad, x_codes ? (const void*)x_codes : x, x_scales, x_type, u, n_tok, pw.d_in, dA, st));
-    TB_TRY(adapter_grad_simt(ad, dy, nullptr, x_type, xa, n_tok, pw.d_out, dB, st));
+    TB_TRY(adapter_grad(ad, x_codes ? (const void*)x_codes : x, x_scales, x_type, u, n_tok, pw.d_in, dA, st));
+    TB_TRY(adapter_grad(ad, dy, nullptr, x_type, xa, n_tok, pw.d_out, dB, st));
   }
   return TB_OK;
 }
