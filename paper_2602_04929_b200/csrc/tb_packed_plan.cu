@@ -4,28 +4,79 @@
 
 namespace tb {
 
-// The tokens of a tile in runs of one adapter.  Tokens without one are in no run.
-__global__ void __launch_bounds__(256) k_adapter_runs(Adapt ad, int n_tok, int n_tile, int4* __restrict__ runs, int* __restrict__ n_runs) {
-  __shared__ int own[257], count[8];
-  const int t0 = blockIdx.x * n_tile, n = min(n_tile, n_tok - t0), i = threadIdx.x;
-  own[i] = i < n ? adapter_of(ad, t0 + i) : -1;
+// What the product kernel wants laid out otherwise, by three kinds of CTAs in one launch: scales and zero-points with the weight rows
+// side by side (a CTA transposes 32 x 32 of them), packed rows on a pitch that TMA takes where theirs is none, and the tokens of
+// every tile in runs of one adapter.
+struct PrepP {
+  PackedW w;
+  Adapt ad;
+  float* st;
+  unsigned *zt, *copy;  // copy: nullptr where the rows are taken as they are
+  int4* runs;
+  int* n_runs;
+  int rows_pad, pitch, n_tok, n_tile, sz_ctas, sz_across, copy_ctas;
+};
+__global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int b = blockIdx.x;
+  if (b < p.sz_ctas) {
+    __shared__ float s[32][33];
+    __shared__ unsigned z[32][33];
+    const int r0 = (b / p.sz_across) * 32, g0 = (b % p.sz_across) * 32;
+    for (int i = warp; i < 32; i += 8) {
+      const int r = r0 + i, g = g0 + lane;
+      const bool in = r < p.w.d_out && g < p.w.n_g;
+      const long long at = (long long)r * p.w.n_g + g;
+      const int zero = in ? p.w.zeros[at] : 0;
+      s[i][lane] = in ? p.w.scales[at] : 0.0f;
+      if (p.w.bits == 8) {
+        z[i][lane] = __float_as_uint((float)(8388608 + zero));
+      } else {
+        const __nv_bfloat162 v = __float2bfloat162_rn((float)(-128 - zero));
+        z[i][lane] = *reinterpret_cast<const unsigned*>(&v);
+      }
+    }
+    __syncthreads();
+    for (int i = warp; i < 32; i += 8)
+      if (g0 + i < p.w.n_g) {  // rows_pad is a multiple of 32
+        p.st[(long long)(g0 + i) * p.rows_pad + r0 + lane] = s[lane][i];
+        p.zt[(long long)(g0 + i) * p.rows_pad + r0 + lane] = z[lane][i];
+      }
+    return;
+  }
+  b -= p.sz_ctas;
+  if (b < p.copy_ctas) {
+    const long long n = (long long)p.w.d_out * p.pitch;
+    for (long long i = (long long)b * 1024 + tid; i < min(n, (long long)(b + 1) * 1024); i += 256) {
+      const int r = (int)(i / p.pitch), k = (int)(i - (long long)r * p.pitch);
+      p.copy[i] = k < p.w.words ? p.w.packed[(long long)r * p.w.words + k] : 0u;
+    }
+    return;
+  }
+  b -= p.copy_ctas;
+  __shared__ int own[257];
+  __shared__ unsigned first[8], change[8];
+  const int t0 = b * p.n_tile, n = min(p.n_tile, p.n_tok - t0);
+  own[tid] = tid < n ? adapter_of(p.ad, t0 + tid) : -1;  // tokens without an adapter are in no run
   __syncthreads();
-  const bool first = own[i] >= 0 && (i == 0 || own[i - 1] != own[i]);
-  const unsigned m = __ballot_sync(0xffffffffu, first);
-  if ((i & 31) == 0) count[i >> 5] = __popc(m);
+  const bool other = tid == 0 || own[tid - 1] != own[tid];
+  const unsigned mf = __ballot_sync(0xffffffffu, other && own[tid] >= 0), mc = __ballot_sync(0xffffffffu, other);
+  if (lane == 0) first[warp] = mf, change[warp] = mc;
   __syncthreads();
-  int at = __popc(m & ((1u << (i & 31)) - 1u)), all = 0;
+  int at = __popc(mf & ((1u << lane) - 1u)), all = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    if (k < (i >> 5)) at += count[k];
-    all += count[k];
+    if (k < warp) at += __popc(first[k]);
+    all += __popc(first[k]);
   }
-  if (first) {
-    int e = i + 1;
-    while (e < n && own[e] == own[i]) ++e;
-    runs[t0 + at] = make_int4(t0 + i, t0 + e, own[i], 0);
+  if (other && own[tid] >= 0) {
+    int e = n, k = warp;
+    unsigned m = lane == 31 ? 0u : change[warp] & ~((2u << lane) - 1u);
+    while (m == 0 && ++k < 8) m = change[k];
+    if (m) e = min(n, 32 * k + __ffs(m) - 1);
+    p.runs[t0 + at] = make_int4(t0 + tid, t0 + e, own[tid], 0);
   }
-  if (i == 0) n_runs[blockIdx.x] = all;
+  if (tid == 0) p.n_runs[b] = all;
 }
 
 // out = the splits' sums, added in their order, rounded once; four values a thread.
@@ -53,7 +104,7 @@ TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
   for (int n_tile = 32; n_tile <= top; n_tile += 32) {
     const int t_tiles = (n_tok + n_tile - 1) / n_tile;
     for (int splits = 1; splits <= 16; ++splits) {
-      const int len = ((n_sum + splits - 1) / splits + 63) / 64 * 64;
+      const int len = ((n_sum + splits - 1) / splits + 127) / 128 * 128;
       if (splits > 1 && (len < 256 || (long long)len * (splits - 1) >= n_sum)) continue;
       const long long tiles = (long long)m_tiles * t_tiles * splits;
       if (tiles > 0x3fffffff) continue;
@@ -71,12 +122,34 @@ TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
   return best;
 }
 
-size_t packed_tc_carve(const TcPlan& t, const Adapt& ad, int n_tok, int n_cols, char* ws, PackedTc* p) {
+size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, char* ws, PackedTc* p) {
   Bump b(ws);
+  p->rows_pad = (w.d_out + 255) / 256 * 256;  // whole tiles of a CTA pair
+  p->pitch = (w.words + 3) / 4 * 4;
+  p->st = b.take<float>((size_t)w.n_g * p->rows_pad);
+  p->zt = b.take<unsigned>((size_t)w.n_g * p->rows_pad);
+  p->words = p->pitch != w.words ? b.take<unsigned>((size_t)w.d_out * p->pitch) : w.packed;
   p->runs = ad.n ? b.take<int4>(n_tok) : nullptr;
   p->n_runs = ad.n ? b.take<int>(t.t_tiles) : nullptr;
   p->part = t.splits > 1 ? b.take<float>((size_t)t.splits * n_tok * n_cols) : nullptr;
   return b.total();
+}
+
+// Rows of 32-bit words, `pitch` words apart.
+static tb_status words_map(CUtensorMap* map, const unsigned* base, int words, int rows, int pitch, int box_words, int box_rows) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return TB_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)words, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch * 4};
+  const cuuint32_t box[2] = {(cuuint32_t)box_words, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  const CUtensorMapSwizzle sw = box_words == 8    ? CU_TENSOR_MAP_SWIZZLE_32B
+                                : box_words == 16 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                : box_words == 32 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                                  : CU_TENSOR_MAP_SWIZZLE_NONE;
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<unsigned*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? TB_OK
+             : TB_ERR_CUDA;
 }
 
 tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat16* in, long long n_tok, __nv_bfloat16* out,
@@ -84,19 +157,26 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   PackedTc p = {};
   p.n_cols = back ? w.d_in : w.d_out, p.n_sum = back ? w.d_out : w.d_in, p.n_tok = (int)n_tok;
   const TcPlan t = packed_tc_plan(p.n_tok, p.n_cols, p.n_sum);
-  packed_tc_carve(t, ad, p.n_tok, p.n_cols, static_cast<char*>(ws), &p);
+  packed_tc_carve(t, w, ad, p.n_tok, p.n_cols, static_cast<char*>(ws), &p);
   p.w = w, p.ad = ad, p.low = low, p.out = out;
   p.M = static_cast<const __nv_bfloat16*>(back ? ad.A : ad.B);
   p.n_tile = t.n_tile, p.m_tiles = t.m_tiles, p.t_tiles = t.t_tiles, p.splits = t.splits, p.split_len = t.split_len;
-  p.group_inv = (1ull << 38) / (unsigned)(w.group / 32) + 1;
-  CUtensorMap map;
-  TB_TRY(make_map_2d(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sizeof(__nv_bfloat16), in, (unsigned long long)p.n_sum,
+  CUtensorMap xmap, wmap;
+  TB_TRY(make_map_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sizeof(__nv_bfloat16), in, (unsigned long long)p.n_sum,
                      (unsigned long long)p.n_tok, 64, (unsigned)(t.n_tile / 2), CU_TENSOR_MAP_SWIZZLE_128B));
-  if (ad.n) {
-    k_adapter_runs<<<t.t_tiles, 256, 0, st>>>(ad, p.n_tok, t.n_tile, const_cast<int4*>(p.runs), const_cast<int*>(p.n_runs));
-    TB_LAUNCH_CHECK();
-  }
-  TB_TRY(back ? packed_tc_backward(p, map, t.pairs, st) : packed_tc_forward(p, map, t.pairs, st));
+  TB_TRY(words_map(&wmap, p.words, w.words, w.d_out, p.pitch, 4 * w.bits, back ? 64 : 128));
+  PrepP q = {};
+  q.w = w, q.ad = ad;
+  q.st = const_cast<float*>(p.st), q.zt = const_cast<unsigned*>(p.zt);
+  q.copy = p.words != w.packed ? const_cast<unsigned*>(p.words) : nullptr;
+  q.runs = const_cast<int4*>(p.runs), q.n_runs = const_cast<int*>(p.n_runs);
+  q.rows_pad = p.rows_pad, q.pitch = p.pitch, q.n_tok = p.n_tok, q.n_tile = t.n_tile;
+  q.sz_across = (w.n_g + 31) / 32;
+  q.sz_ctas = q.sz_across * (p.rows_pad / 32);
+  q.copy_ctas = q.copy ? (int)(((long long)w.d_out * p.pitch + 1023) / 1024) : 0;
+  k_packed_prep<<<(unsigned)(q.sz_ctas + q.copy_ctas + (ad.n ? t.t_tiles : 0)), 256, 0, st>>>(q);
+  TB_LAUNCH_CHECK();
+  TB_TRY(back ? packed_tc_backward(p, xmap, wmap, t.pairs, st) : packed_tc_forward(p, xmap, wmap, t.pairs, st));
   if (t.splits > 1) {
     const long long n4 = (long long)p.n_tok * p.n_cols / 4;
     const long long nb = (n4 + 255) / 256;

@@ -17,8 +17,11 @@
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
 // into the tile as zero and is added by the epilogue to the run's own tokens, so that it reaches no other token.
 //
-// Roles (512 threads): warp 0 TMA, warp 1 MMA (CTA 0 issues for the pair), warps 4-7 decode, warps 8-15 epilogue.  Registers are
-// split 56 / 104 / 176 / 176 over the four warpgroups of a launch at 128 (the sums say no more than the launch has).  Every wait is
+// Roles (640 threads): warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair; that of CTA 1 hands its decoded stages
+// on), warp 2 TMA of the packed words with their zero-points and scales, warps 4-11 decode, two warpgroups in turn, warps 12-19
+// epilogue.  The decode warps have no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor
+// cores, waits for all that its thread has in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are
+// split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).  Every wait is
 // bounded as in the Hessian kernels.
 #pragma once
 
@@ -41,18 +44,23 @@ __device__ __forceinline__ uint64_t smem_desc_k_sw128(uint32_t addr) {
   return d;
 }
 
-// The contraction is taken in accumulations that end where a scale's columns end, or PT_PART columns after their beginning.
+// The contraction is taken in accumulations that end where a scale's columns end, or PT_PART columns (a little less for groups that
+// PT_PART does not divide) after their beginning: `end` of the one under way, `g` its group.
 struct Parts {
-  int group, part;
-  __device__ __forceinline__ Parts(int g) : group(g) {
-    const int n = (g + PT_PART - 1) / PT_PART;
-    part = ((g + n - 1) / n + 31) & ~31;
+  int group, part, g, group_end, end;
+  __device__ __forceinline__ Parts(int gr) : group(gr) {
+    const int n = (gr + PT_PART - 1) / PT_PART;
+    part = ((gr + n - 1) / n + 31) & ~31;
   }
-  __device__ __forceinline__ int end(int k, int k_end) const {  // of the accumulation that has column k
-    const int g = k / group, at = k - g * group;
-    int e = (at / part + 1) * part;
-    if (e > group) e = group;
-    return min(k_end, g * group + e);
+  __device__ __forceinline__ void start(int k) {  // at column k
+    g = k / group;
+    const int g0 = g * group;
+    group_end = g0 + group;
+    end = min(group_end, g0 + ((k - g0) / part + 1) * part);
+  }
+  __device__ __forceinline__ void next() {
+    if (end == group_end) ++g, group_end += group;
+    end = min(group_end, end + part);
   }
 };
 
@@ -72,16 +80,8 @@ __device__ __forceinline__ unsigned field(const unsigned (&w)[N]) {
 __device__ __forceinline__ unsigned bf2(__nv_bfloat162 v) { return *reinterpret_cast<const unsigned*>(&v); }
 __device__ __forceinline__ __nv_bfloat162 bf2(unsigned v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
 
-// A zero-point as the decoders take it.
-struct Zero {
-  __nv_bfloat162 up;  // -(128 + z), twice
-  float f;            // 2^23 + z
-  __device__ __forceinline__ void set(int z) {
-    up = __float2bfloat162_rn((float)(-128 - z));
-    f = (float)(8388608 + z);
-  }
-};
-
+// A zero-point as the decoders take it, made once a call (k_packed_prep): -(128 + z) twice in bf16, or 2^23 + z in float for
+// eight bits.
 // Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
 // is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)
 // is joined with itself 16 - b bits higher.  Eight bits go through float.
@@ -93,29 +93,29 @@ __device__ __forceinline__ unsigned apart(unsigned f) {  // f: N codes; a produc
     return f | (f << (16 - BITS));
 }
 template <int BITS, int C0, int N>
-__device__ __forceinline__ void decode8(const unsigned (&w)[N], const Zero& z, unsigned (&o)[4]) {
+__device__ __forceinline__ void decode8(const unsigned (&w)[N], unsigned z, unsigned (&o)[4]) {
   if constexpr (BITS == 8) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const unsigned v = w[(C0 + 2 * i) >> 2] >> (8 * ((C0 + 2 * i) & 3));
-      const float a = __uint_as_float(0x4B000000u | (v & 0xffu)) - z.f, b = __uint_as_float(0x4B000000u | ((v >> 8) & 0xffu)) - z.f;
+      const float a = __uint_as_float(0x4B000000u | (v & 0xffu)) - __uint_as_float(z), b = __uint_as_float(0x4B000000u | ((v >> 8) & 0xffu)) - __uint_as_float(z);
       o[i] = bf2(__floats2bfloat162_rn(a, b));
     }
   } else if constexpr (BITS <= 4) {
     constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
     const unsigned y0 = apart<BITS, 4>(field<C0 * BITS, 4 * BITS>(w)), y1 = apart<BITS, 4>(field<(C0 + 4) * BITS, 4 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), z.up));
-    o[1] = bf2(__hadd2(bf2(((y0 >> (2 * BITS)) & m) | 0x43004300u), z.up));
-    o[2] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), z.up));
-    o[3] = bf2(__hadd2(bf2(((y1 >> (2 * BITS)) & m) | 0x43004300u), z.up));
+    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(((y0 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
+    o[2] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(((y1 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
   } else {
     constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
     const unsigned y0 = apart<BITS, 2>(field<C0 * BITS, 2 * BITS>(w)), y1 = apart<BITS, 2>(field<(C0 + 2) * BITS, 2 * BITS>(w));
     const unsigned y2 = apart<BITS, 2>(field<(C0 + 4) * BITS, 2 * BITS>(w)), y3 = apart<BITS, 2>(field<(C0 + 6) * BITS, 2 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), z.up));
-    o[1] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), z.up));
-    o[2] = bf2(__hadd2(bf2((y2 & m) | 0x43004300u), z.up));
-    o[3] = bf2(__hadd2(bf2((y3 & m) | 0x43004300u), z.up));
+    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
+    o[1] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
+    o[2] = bf2(__hadd2(bf2((y2 & m) | 0x43004300u), bf2(z)));
+    o[3] = bf2(__hadd2(bf2((y3 & m) | 0x43004300u), bf2(z)));
   }
 }
 
@@ -130,36 +130,40 @@ __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]) : "memory");
 }
 
-// A decoder thread's 64 codes of a stage: one row, 2 BITS words, and the zero-point and scale of either half.
-template <int BITS>
-struct Words {
-  unsigned w[2 * BITS];
-  int z[2];
-  float s[2];
-  __device__ __forceinline__ void load(const unsigned* p, int n, bool wide) {  // n words are inside the row
-    if (wide && n == 2 * BITS) {
-      if constexpr (BITS % 2 == 0) {
-#pragma unroll
-        for (int i = 0; i < BITS / 2; ++i) {
-          const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
-          w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < BITS; ++i) {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(p) + i);
-          w[2 * i] = v.x, w[2 * i + 1] = v.y;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2 * BITS; ++i) w[i] = i < n ? __ldg(p + i) : 0u;
-    }
+// The packed words on their way to the decode warps: 128 columns of the CTA's 128 weight rows (forward, two stages) or of 64 weight
+// rows (backward, one stage), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points, and
+// backward scales.  A ring of STAGES such units.  Rows of 32, 64 and 128 bytes are swizzled, so that neighbouring threads' rows lie
+// in different banks.
+template <int BITS, bool BACK>
+struct Raw {
+  enum {
+    ROWS = BACK ? 64 : 128,
+    ROW = 16 * BITS,
+    Z = ROWS * ROW,
+    S = Z + 4 * ROWS * 4,
+    BYTES = (BACK ? S + 4 * ROWS * 4 : S),
+    PAD = (BYTES + 1023) & ~1023,  // swizzled rows start on a multiple of their pattern
+    MMA_STAGES = BITS <= 4 ? 6 : 5,
+    ROOM = PT_SMEM - 1024 - 512 - MMA_STAGES * PT_STAGE_BYTES,
+    STAGES = ROOM / PAD < 8 ? ROOM / PAD : 8
+  };
+  static_assert(STAGES >= 2, "the ring holds two units at least");
+  // 16-byte piece c of row r
+  static __device__ __forceinline__ uint32_t piece(int r, int c) {
+    if constexpr (ROW == 32) return r * ROW + ((c ^ ((r >> 2) & 1)) << 4);
+    if constexpr (ROW == 64) return r * ROW + ((c ^ ((r >> 1) & 3)) << 4);
+    if constexpr (ROW == 128) return r * ROW + ((c ^ (r & 7)) << 4);
+    return r * ROW + (c << 4);
   }
 };
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 template <int BITS, int C, bool BACK>
-__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const Zero (&z)[2], const float (&s)[2], uint32_t row_addr,
+__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const float (&s)[2], uint32_t row_addr,
                                            uint32_t sw) {
   if constexpr (C < 8) {
     unsigned o[4];
@@ -184,31 +188,42 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
 }
 
 template <int BITS, bool BACK>
-__global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap) {
+__global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+  using Ring = Raw<BITS, BACK>;
+  constexpr int STAGES = Ring::MMA_STAGES;
   extern __shared__ unsigned char pt_smem_raw[];
   const uint32_t raw = smem_u32(pt_smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   unsigned char* gen_base = pt_smem_raw + (base - raw);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_base + PT_STAGES * PT_STAGE_BYTES);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * PT_STAGES + 4);
+  const uint32_t raw_base = base + STAGES * PT_STAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen_base + (PT_SMEM - 1024 - 512));
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 4 + 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* odd_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);  // adapters hold what is not finite (once seen, stays)
   const uint32_t bar0 = smem_u32(bars);
-  // full: in CTA 0, its TMA warp and the decode warps of both CTAs arrive, and the bytes of both; empty, accf: in both, from the
-  // commits of CTA 0; acce: in CTA 0, the epilogue warps of both
+  // full: in CTA 0, its TMA warp and decode warps and the relay of CTA 1 arrive, and the bytes of both; dec: in CTA 1, its decode
+  // warps, for the relay; empty, accf: in both, from the commits of CTA 0; acce: in CTA 0, the epilogue warps of both
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](int s) { return bar0 + 8u * (PT_STAGES + s); };
-  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * PT_STAGES + b); };
-  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * PT_STAGES + 2 + b); };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
+  auto dec_bar = [&](int s) { return bar0 + 8u * (2 * STAGES + s); };
+  auto accf_bar = [&](int b) { return bar0 + 8u * (3 * STAGES + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (3 * STAGES + 2 + b); };
+  auto raw_full = [&](int s) { return bar0 + 8u * (3 * STAGES + 4 + s); };   // a unit's bytes are in the ring
+  auto raw_empty = [&](int s) { return bar0 + 8u * (3 * STAGES + 12 + s); };  // the decode warps that it belongs to have read it
 
   uint32_t rank;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < PT_STAGES; ++s) {
-      mbar_init(full_bar(s), 1 + 8);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full_bar(s), 1 + 4 + 1);
+      mbar_init(dec_bar(s), 4);
       mbar_init(empty_bar(s), 1);
+    }
+    for (int s = 0; s < 8; ++s) {
+      mbar_init(raw_full(s), 1);
+      mbar_init(raw_empty(s), 4);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf_bar(b), 1);
@@ -229,8 +244,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
   const uint32_t tmem_base = *tmem_slot;
   const int half_n = p.n_tile >> 1;
   const int n_tiles = p.m_tiles * p.t_tiles * p.splits;
-  const int group = BACK ? p.n_sum : p.w.group;
-  const Parts parts(group);
+  const int group = BACK ? p.n_sum : p.w.group;  // columns of a scale that leaves the sum
   struct Tile {
     int m0, t0, split, k0, k1, n_runs, lora;
   };
@@ -250,7 +264,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer: this CTA's half of the tokens ----------------
       uint32_t it = 0;
@@ -259,8 +273,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
         const Tile c = tile_of(t);
         const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
         for (int st = 0; st < n_st + c.lora; ++st, ++it) {
-          const int s = it % PT_STAGES;
-          if (!mbar_poll(empty_bar(s), ((it / PT_STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error)) {
+          const int s = it % STAGES;
+          if (!mbar_wait(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error)) {
             ok = false;
             break;
           }
@@ -273,103 +287,213 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           }
         }
       }
-    } else if (warp == 1 && rank == 0 && lane == 0) {
-      // ---------------- MMA issuer (CTA 0) ----------------
+    } else if (warp == 1 && rank == 0) {
+      // ---------------- MMA issuer (CTA 0): the warp goes through the stages together, one lane issues ----------------
       const uint32_t id_main = (1u << 4) | (1u << 7) | (1u << 10) | (BACK ? 1u << 15 : 0u) | ((uint32_t)(p.n_tile >> 3) << 17) | (16u << 24);
       const uint32_t id_lora = id_main | (1u << 15);  // the adapters' matrix is stored along M either way
-      uint32_t it = 0, acc_it = 0;
+      const bool one = elect_one();
+      uint32_t s = 0, phase = 0, acc_it = 0;
+      bool ok = true;
+      // the constant halves of the descriptors; an operand's address goes into the low half, in units of 16 bytes
+      const uint64_t a_main = BACK ? smem_desc_mn_sw128(base) : smem_desc_k_sw128(base), a_lora = smem_desc_mn_sw128(base);
+      const uint64_t b_main = smem_desc_k_sw128(base + PT_A_BYTES);
+      constexpr uint32_t a_step = (BACK ? 2048 : 32) >> 4, l_step = 2048 >> 4, b_step = 32 >> 4;
+      Parts parts(group);
+      auto acc_free = [&]() {
+        const bool got = mbar_wait_warp(acce_bar(acc_it & 1u), ((acc_it >> 1) & 1u) ^ 1u, abort_flag, &g_packed_error);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        return got;
+      };
+      for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+        const Tile c = tile_of(t);
+        const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
+        parts.start(c.k0);
+        int k = c.k0, left = 0, todo = (c.k1 - c.k0 + 15) >> 4;  // column; steps of 16 of the accumulation under way, of the tile
+        for (int st = 0; st < n_st + c.lora; ++st) {
+          ok = mbar_wait_warp(full_bar(s), phase, abort_flag, &g_packed_error);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t at = s * (PT_STAGE_BYTES >> 4);
+          const uint64_t bd = b_main + at;
+          if (st < n_st) {
+            const uint64_t ad = a_main + at;
+            uint32_t more = 1;
+            if (left == 0) {
+              ok = acc_free();
+              if (!ok) break;
+              left = (min(parts.end, c.k1) - k + 15) >> 4;
+              parts.next();
+              more = 0;
+            }
+            if (left >= 4 && todo >= 4) {  // the whole stage in one accumulation
+              const uint32_t d = tmem_base + (acc_it & 1u) * 256u;
+              left -= 4;
+              if (one) {
+                umma_bf16_pair(d, ad, bd, id_main, more);
+                umma_bf16_pair(d, ad + a_step, bd + b_step, id_main, 1);
+                umma_bf16_pair(d, ad + 2 * a_step, bd + 2 * b_step, id_main, 1);
+                umma_bf16_pair(d, ad + 3 * a_step, bd + 3 * b_step, id_main, 1);
+                umma_commit_pair(empty_bar(s));
+                if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
+              }
+              __syncwarp();
+              todo -= 4, k += 64;
+              if (left == 0) ++acc_it;
+            } else {
+              const int steps = min(4, todo);
+              todo -= steps;
+              for (int kk = 0; kk < steps; ++kk) {
+                if (left == 0) {
+                  ok = acc_free();
+                  if (!ok) break;
+                  left = (min(parts.end, c.k1) - k + 15) >> 4;
+                  parts.next();
+                  more = 0;
+                }
+                --left;
+                if (one) {
+                  umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, ad + kk * a_step, bd + kk * b_step, id_main, more);
+                  if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
+                }
+                __syncwarp();
+                more = 1;
+                k += 16;
+                if (left == 0) ++acc_it;
+              }
+              if (!ok) break;
+              if (one) umma_commit_pair(empty_bar(s));
+              __syncwarp();
+            }
+          } else {
+            if (st == n_st) {
+              ok = acc_free();
+              if (!ok) break;
+            }
+            const bool last = st == n_st + c.lora - 1;
+            if (one) {
+#pragma unroll
+              for (int kk = 0; kk < PT_BK / 16; ++kk)
+                umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, a_lora + at + kk * l_step, bd + kk * b_step, id_lora, st == n_st && kk == 0 ? 0u : 1u);
+              umma_commit_pair(empty_bar(s));
+              if (last) umma_commit_pair(accf_bar(acc_it & 1u));
+            }
+            __syncwarp();
+            if (last) ++acc_it;
+          }
+          if (++s == STAGES) s = 0, phase ^= 1u;
+        }
+      }
+    }
+    if (warp == 1 && rank == 1 && lane == 0) {
+      // ---------------- relay (CTA 1): its decoded stages, told to CTA 0 by a thread that has nothing else in flight -----------
+      uint32_t it = 0;
       bool ok = true;
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
         const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
-        int end = 0;  // of the accumulation under way
         for (int st = 0; st < n_st + c.lora && ok; ++st, ++it) {
-          const int s = it % PT_STAGES;
-          ok = mbar_poll_cluster(full_bar(s), (it / PT_STAGES) & 1u, abort_flag, &g_packed_error);
+          const int s = it % STAGES;
+          ok = mbar_wait(dec_bar(s), (it / STAGES) & 1u, abort_flag, &g_packed_error);
+          if (ok) mbar_arrive_remote(map_to_rank(full_bar(s), 0));
+        }
+      }
+    } else if (warp == 2 && lane == 0) {
+      // ---------------- TMA producer of the packed words, zero-points and scales ----------------
+      const int G = p.w.group >> 5, last = (p.w.d_in >> 5) - 1;  // runs of 32 columns with one scale; the last run
+      const int n_sz = p.w.group % 128 == 0 ? 1 : 4;             // one zero-point (and scale) for a unit's four runs, or each its own
+      const uint32_t bytes = Ring::Z + n_sz * Ring::ROWS * (BACK ? 8u : 4u);
+      uint32_t s = 0, phase = 1;
+      bool ok = true;
+      for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+        const Tile c = tile_of(t);
+        const int n_u = BACK ? (c.k1 - c.k0 + 63) / 64 : (c.k1 - c.k0 + 127) / 128;
+        for (int u = 0; u < n_u; ++u) {
+          ok = mbar_wait(raw_empty(s), phase, abort_flag, &g_packed_error);
           if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t sa = base + s * PT_STAGE_BYTES, sb = sa + PT_A_BYTES;
-          const bool lora = st >= n_st;
-#pragma unroll
-          for (int kk = 0; kk < PT_BK / 16; ++kk) {
-            const int k = c.k0 + st * PT_BK + kk * 16;
-            if (!lora && k >= c.k1) break;
-            const bool first = lora ? (st == n_st && kk == 0) : (k == c.k0 || k >= end);
-            const uint32_t b = acc_it & 1u;
-            if (first) {
-              ok = mbar_poll_cluster(acce_bar(b), ((acc_it >> 1) & 1u) ^ 1u, abort_flag, &g_packed_error);
-              if (!ok) break;
-              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-              if (!lora) end = parts.end(k, c.k1);
-            }
-            const uint64_t ad = BACK || lora ? smem_desc_mn_sw128(sa + kk * 2048) : smem_desc_k_sw128(sa + kk * 32);
-            umma_bf16_pair(tmem_base + b * 256u, ad, smem_desc_k_sw128(sb + kk * 32), lora ? id_lora : id_main, first ? 0u : 1u);
-            if (lora ? (st == n_st + c.lora - 1 && kk == PT_BK / 16 - 1) : k + 16 >= end) {
-              umma_commit_pair(accf_bar(b));
-              ++acc_it;
-            }
+          const uint32_t dst = raw_base + s * Ring::PAD;
+          const int r = BACK ? c.k0 + 64 * u : c.m0, j = BACK ? c.m0 : c.k0 + 128 * u;
+          mbar_expect_tx(raw_full(s), bytes);
+          tma_load_2d(dst, &wmap, (j >> 5) * BITS, r, raw_full(s));
+          for (int h = 0; h < n_sz; ++h) {
+            const long long at = (long long)(min((j >> 5) + h, last) / G) * p.rows_pad + r;
+            bulk_load(dst + Ring::Z + h * Ring::ROWS * 4, p.zt + at, Ring::ROWS * 4, raw_full(s));
+            if (BACK) bulk_load(dst + Ring::S + h * Ring::ROWS * 4, p.st + at, Ring::ROWS * 4, raw_full(s));
           }
-          if (ok) umma_commit_pair(empty_bar(s));
+          if (++s == Ring::STAGES) s = 0, phase ^= 1u;
         }
       }
     }
-  } else if (warp < 8) {
+  } else if (warp < 12) {
     // ---------------- decode: operand A of this CTA ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    const int tid = threadIdx.x - 128;
-    // forward: thread = tile row (a weight row), 64 contraction columns; backward: 64 weight rows x two halves of the columns
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const int tid = (threadIdx.x - 128) & 127, turn = (warp - 4) >> 2;  // two warpgroups take turns at the stages
+    // forward: thread = tile row (a weight row), 64 contraction columns of a stage; backward: 64 weight rows x two halves
     const int my_row = BACK ? tid & 63 : tid;
     const uint32_t row_off = BACK ? (uint32_t)(tid >> 6) * 8192u + (uint32_t)my_row * 128u : (uint32_t)my_row * 128u;
     const uint32_t sw = (uint32_t)(my_row & 7);
-    const bool wide = p.w.d_in % 64 == 0;
-    uint32_t it = 0;
+    const bool one_sz = p.w.group % 128 == 0;
+    constexpr int PER = BACK ? 1 : 2;  // stages of a unit
+    uint32_t it = 0, unit = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile c = tile_of(t);
       const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
-      // first code of this thread at stage st: row r, column j
-      auto place = [&](int st, int& r, int& j) {
-        r = BACK ? c.k0 + st * PT_BK + my_row : c.m0 + my_row;
-        j = BACK ? c.m0 + 64 * (tid >> 6) : c.k0 + st * PT_BK;
-      };
-      auto fetch = [&](int st, Words<BITS>& wd) {
-        int r, j;
-        place(st, r, j);
-        const int left = r < p.w.d_out && st < n_st ? min(64, p.w.d_in - j) : 0;
-        wd.load(p.w.packed + (long long)r * p.w.words + (j >> 5) * BITS, left > 0 ? left / 32 * BITS : 0, wide);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // outside, the words are zeros: any zero-point gives finite values, which meet zeros or are not stored
-          const bool in = left > 32 * h;
-          const long long at = (long long)r * p.w.n_g + (int)(((unsigned long long)((j >> 5) + h) * p.group_inv) >> 38);
-          wd.z[h] = in ? __ldg(p.w.zeros + at) : 0;
-          wd.s[h] = BACK && in ? __ldg(p.w.scales + at) : 0.0f;
+      for (int st = 0; st < n_st && ok; st += PER, ++unit) {
+        const int here = min(PER, n_st - st);
+        if ((int)(unit & 1u) != turn) {
+          it += here;
+          continue;
         }
-      };
-      Words<BITS> nxt;
-      fetch(0, nxt);
-      for (int st = 0; st < n_st && ok; ++st, ++it) {
-        const int s = it % PT_STAGES;
-        const Words<BITS> cur = nxt;
-        fetch(st + 1, nxt);
-        Zero z[2];
-        z[0].set(cur.z[0]), z[1].set(cur.z[1]);
-        int okw = 1;
-        if (lane == 0) okw = mbar_poll(empty_bar(s), ((it / PT_STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error) ? 1 : 0;
-        ok = __shfl_sync(0xffffffffu, okw, 0) != 0;
+        const uint32_t rs = unit % Ring::STAGES;
+        ok = mbar_wait_warp(raw_full(rs), (unit / Ring::STAGES) & 1u, abort_flag, &g_packed_error);
         if (!ok) break;
-        decode_row<BITS, 0, BACK>(cur.w, z, cur.s, base + s * PT_STAGE_BYTES + row_off, sw);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive_remote(map_to_rank(full_bar(s), 0));
+        const unsigned char* q = gen_base + (raw_base - base) + rs * Ring::PAD;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          if (i >= here) break;
+          // outside the matrix the words are zeros and any zero-point gives finite values, which meet zeros or are not stored
+          const int half = BACK ? tid >> 6 : i;  // of the unit's 128 columns
+          unsigned w[2 * BITS], z[2];
+          float sc[2] = {0.0f, 0.0f};
+          if constexpr (BITS % 2 == 0) {
+#pragma unroll
+            for (int e = 0; e < BITS / 2; ++e) {
+              const uint4 v = *reinterpret_cast<const uint4*>(q + Ring::piece(my_row, half * (BITS / 2) + e));
+              w[4 * e] = v.x, w[4 * e + 1] = v.y, w[4 * e + 2] = v.z, w[4 * e + 3] = v.w;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < BITS; ++e) {
+              const uint2 v = *reinterpret_cast<const uint2*>(q + my_row * Ring::ROW + half * 8 * BITS + 8 * e);
+              w[2 * e] = v.x, w[2 * e + 1] = v.y;
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int o = (one_sz ? 0 : 2 * half + h) * Ring::ROWS * 4 + my_row * 4;
+            z[h] = *reinterpret_cast<const unsigned*>(q + Ring::Z + o);
+            if (BACK) sc[h] = *reinterpret_cast<const float*>(q + Ring::S + o);
+          }
+          if (i == here - 1) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(raw_empty(rs));
+          }
+          const int s = it % STAGES;
+          ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
+          if (!ok) break;
+          decode_row<BITS, 0, BACK>(w, z, sc, base + s * PT_STAGE_BYTES + row_off, sw);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(rank == 0 ? full_bar(s) : dec_bar(s));
+          ++it;
+        }
       }
       // the adapters: four slots a stage, slot = (run, 16 of the rank, piece)
       const int n_slots = c.n_runs * nb * 2;
       for (int st = 0; st < c.lora && ok; ++st, ++it) {
-        const int s = it % PT_STAGES;
-        int okw = 1;
-        if (lane == 0) okw = mbar_poll(empty_bar(s), ((it / PT_STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error) ? 1 : 0;
-        ok = __shfl_sync(0xffffffffu, okw, 0) != 0;
+        if ((int)(it & 1u) != turn) continue;
+        const int s = it % STAGES;
+        ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
         if (!ok) break;
         const uint32_t sa = base + s * PT_STAGE_BYTES, sb = sa + PT_A_BYTES;
         {
@@ -430,13 +554,14 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(map_to_rank(full_bar(s), 0));
+        if (lane == 0) mbar_arrive(rank == 0 ? full_bar(s) : dec_bar(s));
       }
     }
   } else {
     // ---------------- epilogue: 128 columns (TMEM lanes), half of the tokens each ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-    const int q = warp & 3, hf = (warp - 8) >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    const int q = warp & 3, hf = (warp - 12) >> 2;
+    Parts parts(group);
     uint32_t acc_it = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
@@ -445,7 +570,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       float run[128];
 #pragma unroll
       for (int i = 0; i < 128; ++i) run[i] = 0.0f;
-      const float* srow = p.w.scales + (long long)min(col, p.w.d_out - 1) * p.w.n_g;
+      parts.start(c.k0);
       int k = c.k0;
       bool lora = false;
       while (ok) {
@@ -454,62 +579,61 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           lora = true;
         }
         float s = 1.0f;
-        if (!BACK && !lora) s = __ldg(srow + k / group);
+        if (!BACK && !lora) s = __ldg(p.st + (long long)parts.g * p.rows_pad + col);
         const uint32_t b = acc_it & 1u;
-        int okw = 1;
-        if (lane == 0) okw = mbar_poll(accf_bar(b), (acc_it >> 1) & 1u, abort_flag, &g_packed_error) ? 1 : 0;
-        ok = __shfl_sync(0xffffffffu, okw, 0) != 0;
+        ok = mbar_wait_warp(accf_bar(b), (acc_it >> 1) & 1u, abort_flag, &g_packed_error);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256u + (uint32_t)(hf * half_n);
 #pragma unroll
         for (int ch = 0; ch < 8; ++ch) {
-          if (16 * ch < half_n) {
-            uint32_t r[16];
-            tmem_ld_32x16(taddr + ch * 16, r);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (16 * ch >= half_n) break;
+          uint32_t r[16];
+          tmem_ld_32x16(taddr + ch * 16, r);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
-          }
+          for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive_remote(map_to_rank(acce_bar(b), 0));
+        if (lane == 0) mbar_arrive_remote_relaxed(map_to_rank(acce_bar(b), 0));
         ++acc_it;
-        if (!lora) k = parts.end(k, c.k1);
+        if (!lora) k = parts.end, parts.next();
       }
       if (!ok) break;
-      const int tok0 = c.t0 + hf * half_n;
-      if (c.lora && *odd_flag) {
-        // (set before the adapters' last stage was handed over, hence before its accumulation was complete)
-        if (col < p.n_cols)
-          for (int u = 0; u < c.n_runs; ++u) {
-            const int4 ru = p.runs[c.t0 + u];
-            const float f = p.ad.scale[ru.z];
-            for (int r = 0; r < p.ad.rank; ++r) {
-              const float m = __bfloat162float(p.M[((long long)ru.z * p.ad.rank + r) * p.n_cols + col]);
-              if (fabsf(m) <= 3.4028234e38f) continue;
+      const int tok0 = c.t0 + hf * half_n, n = min(half_n, p.n_tok - tok0);  // this warp's tokens
+      if (col >= p.n_cols || n <= 0) continue;
+      const long long at = (long long)tok0 * p.n_cols + col;
+      float* fo = p.part + (long long)c.split * p.n_tok * p.n_cols + at;
+      __nv_bfloat16* bo = p.out + at;
+      if (p.splits > 1) {
 #pragma unroll
-              for (int i = 0; i < 128; ++i) {
-                const int tok = tok0 + i;
-                if (i < half_n && tok >= ru.x && tok < ru.y) run[i] = fmaf(f * p.low[(long long)tok * p.ad.rank + r], m, run[i]);
-              }
+        for (int i = 0; i < 128; ++i)
+          if (i < n) fo[i * p.n_cols] = run[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (i < n) bo[i * p.n_cols] = __float2bfloat16(run[i]);
+      }
+      // what is not finite in the adapters' rows, to the tokens that it belongs to: whatever finite value was stored there stops
+      // being one.  (The flag was set before the adapters' last stage was handed over, hence before its accumulation was complete.)
+      if (c.lora && *odd_flag)
+        for (int u = 0; u < c.n_runs; ++u) {
+          const int4 ru = p.runs[c.t0 + u];
+          const float f = p.ad.scale[ru.z];
+          for (int r = 0; r < p.ad.rank; ++r) {
+            const float m = __bfloat162float(p.M[((long long)ru.z * p.ad.rank + r) * p.n_cols + col]);
+            if (fabsf(m) <= 3.4028234e38f) continue;
+            for (int tok = max(ru.x, tok0); tok < min(ru.y, tok0 + n); ++tok) {
+              const float v = f * p.low[(long long)tok * p.ad.rank + r] * m;
+              const long long i = (long long)(tok - tok0) * p.n_cols;
+              if (p.splits > 1)
+                fo[i] += v;
+              else
+                bo[i] = __float2bfloat16(__bfloat162float(bo[i]) + v);
             }
           }
-      }
-      if (col < p.n_cols) {
-        if (p.splits > 1) {
-          float* o = p.part + ((long long)c.split * p.n_tok + tok0) * p.n_cols + col;
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i < half_n && tok0 + i < p.n_tok) o[(long long)i * p.n_cols] = run[i];
-        } else {
-          __nv_bfloat16* o = p.out + (long long)tok0 * p.n_cols + col;
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i < half_n && tok0 + i < p.n_tok) o[(long long)i * p.n_cols] = __float2bfloat16(run[i]);
         }
-      }
     }
   }
 
@@ -524,7 +648,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
 namespace tb {
 
 template <int BITS, bool BACK>
-tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& map, int pairs, cudaStream_t st) {
+tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& xmap, const CUtensorMap& wmap, int pairs, cudaStream_t st) {
   static bool configured[64] = {false};
   int dev = 0;
   TB_CUDA_CHECK(cudaGetDevice(&dev));
@@ -532,7 +656,7 @@ tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& map, int pairs,
   if (!configured[dev]) {
     cudaFuncAttributes at;
     TB_CUDA_CHECK(cudaFuncGetAttributes(&at, k_packed_tc<BITS, BACK>));
-    if (at.numRegs != 128) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 128 registers a thread has
+    if (at.numRegs != 96) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 96 registers a thread has
     TB_CUDA_CHECK(cudaFuncSetAttribute(k_packed_tc<BITS, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PT_SMEM));
     configured[dev] = true;
   }
@@ -548,21 +672,21 @@ tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& map, int pairs,
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_packed_tc<BITS, BACK>, p, map));
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_packed_tc<BITS, BACK>, p, xmap, wmap));
   TB_LAUNCH_CHECK();
   return TB_OK;
 }
 
 template <bool BACK>
-tb_status launch_packed_tc_bits(const PackedTc& p, const CUtensorMap& map, int pairs, cudaStream_t st) {
+tb_status launch_packed_tc_bits(const PackedTc& p, const CUtensorMap& xmap, const CUtensorMap& wmap, int pairs, cudaStream_t st) {
   switch (p.w.bits) {
-    case 2: return launch_packed_tc<2, BACK>(p, map, pairs, st);
-    case 3: return launch_packed_tc<3, BACK>(p, map, pairs, st);
-    case 4: return launch_packed_tc<4, BACK>(p, map, pairs, st);
-    case 5: return launch_packed_tc<5, BACK>(p, map, pairs, st);
-    case 6: return launch_packed_tc<6, BACK>(p, map, pairs, st);
-    case 7: return launch_packed_tc<7, BACK>(p, map, pairs, st);
-    default: return launch_packed_tc<8, BACK>(p, map, pairs, st);
+    case 2: return launch_packed_tc<2, BACK>(p, xmap, wmap, pairs, st);
+    case 3: return launch_packed_tc<3, BACK>(p, xmap, wmap, pairs, st);
+    case 4: return launch_packed_tc<4, BACK>(p, xmap, wmap, pairs, st);
+    case 5: return launch_packed_tc<5, BACK>(p, xmap, wmap, pairs, st);
+    case 6: return launch_packed_tc<6, BACK>(p, xmap, wmap, pairs, st);
+    case 7: return launch_packed_tc<7, BACK>(p, xmap, wmap, pairs, st);
+    default: return launch_packed_tc<8, BACK>(p, xmap, wmap, pairs, st);
   }
 }
 

@@ -3,8 +3,8 @@
 
 namespace tb {
 
-tb_status packed_tc_backward(const PackedTc& p, const CUtensorMap& map, int pairs, cudaStream_t st) {
-  return launch_packed_tc_bits<true>(p, map, pairs, st);
+tb_status packed_tc_backward(const PackedTc& p, const CUtensorMap& xmap, const CUtensorMap& wmap, int pairs, cudaStream_t st) {
+  return launch_packed_tc_bits<true>(p, xmap, wmap, pairs, st);
 }
 
 int packed_bwd_error_read_clear() { return packed_tc_error_read_clear(); }

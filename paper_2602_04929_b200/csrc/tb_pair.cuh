@@ -37,6 +37,11 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// The same without a release: where the arrival only says that tensor memory has been read (tcgen05.wait::ld came before).
+// A release at cluster scope makes the thread wait for every access it has in flight.
+__device__ __forceinline__ void mbar_arrive_remote_relaxed(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // Bounded wait that polls without suspending: for barriers completed from the other CTA of the pair
 // (a remote arrive, or a commit sent to both CTAs).
 __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
@@ -63,30 +68,9 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatil
   }
   return true;
 }
-// The same with acquire at cluster scope: for barriers whose arrivals hand over what the partner CTA's threads wrote.
-__device__ __forceinline__ bool mbar_test_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_poll_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* device_error_word) {
-  if (mbar_test_wait_cluster(bar, parity)) return true;
-  const long long t0 = clock64();
-  while (!mbar_test_wait_cluster(bar, parity)) {
-    if (*abort_flag) return false;
-    if (clock64() - t0 > MBAR_WAIT_BUDGET) {
-      *abort_flag = 1;
-      atomicExch(device_error_word, 1);
-      return false;
-    }
-  }
-  return true;
+// mbar_wait by a whole warp, which goes on or gives up together
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* device_error_word) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, device_error_word));
 }
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
