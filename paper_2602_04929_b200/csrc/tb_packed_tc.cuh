@@ -17,8 +17,7 @@
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
 // into the tile as zero and is added by the epilogue to the run's own tokens, so that it reaches no other token.
 //
-// Roles (640 threads): warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair; that of CTA 1 hands its decoded stages
-// on), warp 2 TMA of the packed words with their zero-points and scales, warps 4-11 decode, two warpgroups in turn, warps 12-19
+// Roles (640 threads): warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and scales, warps 4-11 decode, two warpgroups in turn, warps 12-19
 // epilogue.  The decode warps have no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor
 // cores, waits for all that its thread has in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are
 // split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).  Every wait is
@@ -197,19 +196,18 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
   unsigned char* gen_base = pt_smem_raw + (base - raw);
   const uint32_t raw_base = base + STAGES * PT_STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(gen_base + (PT_SMEM - 1024 - 512));
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 4 + 16);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4 + 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* odd_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);  // adapters hold what is not finite (once seen, stays)
   const uint32_t bar0 = smem_u32(bars);
-  // full: in CTA 0, its TMA warp and decode warps and the relay of CTA 1 arrive, and the bytes of both; dec: in CTA 1, its decode
-  // warps, for the relay; empty, accf: in both, from the commits of CTA 0; acce: in CTA 0, the epilogue warps of both
+  // full: in CTA 0, its TMA warp and the decode warps of both CTAs (four a stage each) arrive, and the bytes of both; empty, accf: in
+  // both, from the commits of CTA 0; acce: in CTA 0, the epilogue warps of both
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
-  auto dec_bar = [&](int s) { return bar0 + 8u * (2 * STAGES + s); };
-  auto accf_bar = [&](int b) { return bar0 + 8u * (3 * STAGES + b); };
-  auto acce_bar = [&](int b) { return bar0 + 8u * (3 * STAGES + 2 + b); };
-  auto raw_full = [&](int s) { return bar0 + 8u * (3 * STAGES + 4 + s); };   // a unit's bytes are in the ring
-  auto raw_empty = [&](int s) { return bar0 + 8u * (3 * STAGES + 12 + s); };  // the decode warps that it belongs to have read it
+  auto accf_bar = [&](int b) { return bar0 + 8u * (2 * STAGES + b); };
+  auto acce_bar = [&](int b) { return bar0 + 8u * (2 * STAGES + 2 + b); };
+  auto raw_full = [&](int s) { return bar0 + 8u * (2 * STAGES + 4 + s); };   // a unit's bytes are in the ring
+  auto raw_empty = [&](int s) { return bar0 + 8u * (2 * STAGES + 12 + s); };  // the decode warps that it belongs to have read it
 
   uint32_t rank;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -217,8 +215,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(full_bar(s), 1 + 4 + 1);
-      mbar_init(dec_bar(s), 4);
+      mbar_init(full_bar(s), 1 + 8);
       mbar_init(empty_bar(s), 1);
     }
     for (int s = 0; s < 8; ++s) {
@@ -384,20 +381,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
         }
       }
     }
-    if (warp == 1 && rank == 1 && lane == 0) {
-      // ---------------- relay (CTA 1): its decoded stages, told to CTA 0 by a thread that has nothing else in flight -----------
-      uint32_t it = 0;
-      bool ok = true;
-      for (int t = pair; t < n_tiles && ok; t += n_pairs) {
-        const Tile c = tile_of(t);
-        const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
-        for (int st = 0; st < n_st + c.lora && ok; ++st, ++it) {
-          const int s = it % STAGES;
-          ok = mbar_wait(dec_bar(s), (it / STAGES) & 1u, abort_flag, &g_packed_error);
-          if (ok) mbar_arrive_remote(map_to_rank(full_bar(s), 0));
-        }
-      }
-    } else if (warp == 2 && lane == 0) {
+    if (warp == 2 && lane == 0) {
       // ---------------- TMA producer of the packed words, zero-points and scales ----------------
       const int G = p.w.group >> 5, last = (p.w.d_in >> 5) - 1;  // runs of 32 columns with one scale; the last run
       const int n_sz = p.w.group % 128 == 0 ? 1 : 4;             // one zero-point (and scale) for a unit's four runs, or each its own
@@ -484,7 +468,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           decode_row<BITS, 0, BACK>(w, z, sc, base + s * PT_STAGE_BYTES + row_off, sw);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(rank == 0 ? full_bar(s) : dec_bar(s));
+          if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
           ++it;
         }
       }
@@ -554,7 +538,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(rank == 0 ? full_bar(s) : dec_bar(s));
+        if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
       }
     }
   } else {
