@@ -35,6 +35,7 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
   uint32_t rank, cs;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
+  pdl_trigger();  // a product that only needs these sums at its end may start beside
   const int t0 = (blockIdx.x / cs) * TT, r0 = blockIdx.z * 64;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x < TT) own[threadIdx.x] = t0 + (int)threadIdx.x < n_tok ? adapter_of(ad, t0 + threadIdx.x) : -2;

@@ -1,0 +1,66 @@
+// Packed codes to bf16 integers c - z, exact for |c - z| <= 256.
+#pragma once
+
+#include "tb_common.cuh"
+
+namespace tb {
+
+// Field of NB bits from bit POS of the words on.
+template <int POS, int NB, int N>
+__device__ __forceinline__ unsigned field(const unsigned (&w)[N]) {
+  constexpr int i = POS >> 5, s = POS & 31;
+  unsigned v;
+  if constexpr (s + NB <= 32)
+    v = w[i] >> s;
+  else
+    v = __funnelshift_r(w[i], w[i + 1], s);
+  if constexpr (NB < 32) v &= (1u << NB) - 1u;
+  return v;
+}
+
+__device__ __forceinline__ unsigned bf2(__nv_bfloat162 v) { return *reinterpret_cast<const unsigned*>(&v); }
+__device__ __forceinline__ __nv_bfloat162 bf2(unsigned v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
+
+// A zero-point as the decoders take it: -(128 + z) twice in bf16, or 2^23 + z in float for eight bits.
+__device__ __forceinline__ unsigned zero_word(int z, int bits) {
+  if (bits == 8) return __float_as_uint((float)(8388608 + z));
+  return bf2(__float2bfloat162_rn((float)(-128 - z)));
+}
+// Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
+// is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)
+// is joined with itself 16 - b bits higher.  Eight bits go through float.
+template <int BITS, int N>
+__device__ __forceinline__ unsigned apart(unsigned f) {  // f: N codes; a product where the two do not overlap, else an or
+  if constexpr (N * BITS <= 16 - BITS)
+    return f * (1u + (1u << (16 - BITS)));
+  else
+    return f | (f << (16 - BITS));
+}
+template <int BITS, int C0, int N>
+__device__ __forceinline__ void decode8(const unsigned (&w)[N], unsigned z, unsigned (&o)[4]) {
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned v = w[(C0 + 2 * i) >> 2] >> (8 * ((C0 + 2 * i) & 3));
+      const float a = __uint_as_float(0x4B000000u | (v & 0xffu)) - __uint_as_float(z), b = __uint_as_float(0x4B000000u | ((v >> 8) & 0xffu)) - __uint_as_float(z);
+      o[i] = bf2(__floats2bfloat162_rn(a, b));
+    }
+  } else if constexpr (BITS <= 4) {
+    constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
+    const unsigned y0 = apart<BITS, 4>(field<C0 * BITS, 4 * BITS>(w)), y1 = apart<BITS, 4>(field<(C0 + 4) * BITS, 4 * BITS>(w));
+    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(((y0 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
+    o[2] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(((y1 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
+  } else {
+    constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
+    const unsigned y0 = apart<BITS, 2>(field<C0 * BITS, 2 * BITS>(w)), y1 = apart<BITS, 2>(field<(C0 + 2) * BITS, 2 * BITS>(w));
+    const unsigned y2 = apart<BITS, 2>(field<(C0 + 4) * BITS, 2 * BITS>(w)), y3 = apart<BITS, 2>(field<(C0 + 6) * BITS, 2 * BITS>(w));
+    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
+    o[1] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
+    o[2] = bf2(__hadd2(bf2((y2 & m) | 0x43004300u), bf2(z)));
+    o[3] = bf2(__hadd2(bf2((y3 & m) | 0x43004300u), bf2(z)));
+  }
+}
+
+}  // namespace tb

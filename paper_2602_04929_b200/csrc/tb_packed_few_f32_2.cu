@@ -1,0 +1,8 @@
+// y = x Q^T, tokens by the 16, float: the kernel for every width of code.
+#include "tb_packed_few.cuh"
+
+namespace tb {
+
+tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st) { return launch_few_bits<2, 3, float>(p, st); }
+
+}  // namespace tb

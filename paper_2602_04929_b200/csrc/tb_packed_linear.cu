@@ -1,4 +1,5 @@
 // Products with bit-packed weights, low-rank adapters of many requests beside them, and their gradients: the entry points.
+#include "tb_packed_few.cuh"
 #include "tb_packed_plan.cuh"
 
 namespace tb {
@@ -70,6 +71,18 @@ static tb_status checked(const tb_packed_weight* w, const tb_adapters* a, tb_dty
   return TB_OK;
 }
 
+tb_status packed_few_bf16_1(const PackedFew& p, cudaStream_t st);
+tb_status packed_few_bf16_2(const PackedFew& p, cudaStream_t st);
+tb_status packed_few_f32_1(const PackedFew& p, cudaStream_t st);
+tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
+
+// Which product: few tokens in bf16, and float whatever their number, read the weights into registers; more go to tcgen05 tiles, whose
+// smallest has 32 tokens.  The gradient of float inputs runs on the FP32 pipe.
+enum { FEW_TOKENS = 16 };
+static bool takes_few(tb_dtype type, long long n_tok, bool back) {
+  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= 65535ll * FEW_TOKENS);
+}
+
 // Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.
 struct Scratch {
   float* u;
@@ -81,7 +94,7 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
   Bump b(ws);
   s.u = back && ad.n ? b.take<float>((size_t)n_tok * ad.rank) : nullptr;
   size_t n = 0;
-  if (type == TB_BF16) {
+  if (type == TB_BF16 && !takes_few(type, n_tok, back)) {
     PackedTc p;
     const int cols = back ? w.d_in : w.d_out;
     n = packed_tc_carve(packed_tc_plan((int)n_tok, cols, back ? w.d_out : w.d_in), w, ad, (int)n_tok, cols, nullptr, &p);
@@ -93,6 +106,12 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
 
 static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out, const float* low,
                          bool back, void* ws, cudaStream_t st) {
+  if (takes_few(type, n_tok, back)) {
+    PackedFew p;
+    p.w = w, p.ad = ad, p.x = in, p.M = ad.B, p.low = low, p.out = out, p.n_tok = (int)n_tok;
+    if (type == TB_BF16) return n_tok <= 8 ? packed_few_bf16_1(p, st) : packed_few_bf16_2(p, st);
+    return n_tok <= 8 ? packed_few_f32_1(p, st) : packed_few_f32_2(p, st);
+  }
   if (type == TB_BF16)
     return packed_product_tc(w, ad, static_cast<const __nv_bfloat16*>(in), n_tok, static_cast<__nv_bfloat16*>(out), low, back, ws, st);
   return packed_product_simt(w, ad, in, type, n_tok, out, low, back, st);

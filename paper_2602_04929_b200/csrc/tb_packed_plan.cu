@@ -1,5 +1,6 @@
 // Host side of the tensor-core product with bit-packed weights: tiles and splits, the runs of tokens with one adapter, and the
 // sum of the splits.
+#include "tb_packed_decode.cuh"
 #include "tb_packed_plan.cuh"
 
 namespace tb {
@@ -29,12 +30,7 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
       const long long at = (long long)r * p.w.n_g + g;
       const int zero = in ? p.w.zeros[at] : 0;
       s[i][lane] = in ? p.w.scales[at] : 0.0f;
-      if (p.w.bits == 8) {
-        z[i][lane] = __float_as_uint((float)(8388608 + zero));
-      } else {
-        const __nv_bfloat162 v = __float2bfloat162_rn((float)(-128 - zero));
-        z[i][lane] = *reinterpret_cast<const unsigned*>(&v);
-      }
+      z[i][lane] = zero_word(zero, p.w.bits);
     }
     __syncthreads();
     for (int i = warp; i < 32; i += 8)
@@ -79,13 +75,32 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
   if (tid == 0) p.n_runs[b] = all;
 }
 
-// out = the splits' sums, added in their order, rounded once; four values a thread.
-__global__ void __launch_bounds__(256) k_packed_join(const float4* __restrict__ part, uint2* __restrict__ out, long long n4, int splits) {
+// out = the splits' sums, added in their order, and the adapters' share of the token, rounded once; four columns a thread.
+__global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* out, long long n4, int cols4, int splits, const Adapt ad,
+                                                     const float* low, const __nv_bfloat16* M) {
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n4; i += gridDim.x * 256ll) {
     float4 s = __ldcs(part + i);
     for (int k = 1; k < splits; ++k) {
       const float4 v = __ldcs(part + k * n4 + i);
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    if (ad.n) {
+      const long long t = i / cols4;
+      const int id = adapter_of(ad, t);
+      if (id >= 0) {
+        const uint2* m = reinterpret_cast<const uint2*>(M) + (long long)id * ad.rank * cols4 + (i - t * cols4);
+        const float* l = low + t * ad.rank;
+        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+        for (int r = 0; r < ad.rank; ++r) {
+          const uint2 w = __ldg(m + (long long)r * cols4);
+          const float v = l[r];
+          a.x = fmaf(v, __uint_as_float(w.x << 16), a.x), a.y = fmaf(v, __uint_as_float(w.x & 0xffff0000u), a.y);
+          a.z = fmaf(v, __uint_as_float(w.y << 16), a.z), a.w = fmaf(v, __uint_as_float(w.y & 0xffff0000u), a.w);
+        }
+        const float f = ad.scale[id];
+        s.x = fmaf(f, a.x, s.x), s.y = fmaf(f, a.y, s.y), s.z = fmaf(f, a.z, s.z), s.w = fmaf(f, a.w, s.w);
+      }
     }
     const __nv_bfloat162 a = __floats2bfloat162_rn(s.x, s.y), b = __floats2bfloat162_rn(s.z, s.w);
     out[i] = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
@@ -129,8 +144,8 @@ size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n
   p->st = b.take<float>((size_t)w.n_g * p->rows_pad);
   p->zt = b.take<unsigned>((size_t)w.n_g * p->rows_pad);
   p->words = p->pitch != w.words ? b.take<unsigned>((size_t)w.d_out * p->pitch) : w.packed;
-  p->runs = ad.n ? b.take<int4>(n_tok) : nullptr;
-  p->n_runs = ad.n ? b.take<int>(t.t_tiles) : nullptr;
+  p->runs = ad.n && t.splits == 1 ? b.take<int4>(n_tok) : nullptr;
+  p->n_runs = ad.n && t.splits == 1 ? b.take<int>(t.t_tiles) : nullptr;
   p->part = t.splits > 1 ? b.take<float>((size_t)t.splits * n_tok * n_cols) : nullptr;
   return b.total();
 }
@@ -174,13 +189,14 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   q.sz_across = (w.n_g + 31) / 32;
   q.sz_ctas = q.sz_across * (p.rows_pad / 32);
   q.copy_ctas = q.copy ? (int)(((long long)w.d_out * p.pitch + 1023) / 1024) : 0;
-  k_packed_prep<<<(unsigned)(q.sz_ctas + q.copy_ctas + (ad.n ? t.t_tiles : 0)), 256, 0, st>>>(q);
+  k_packed_prep<<<(unsigned)(q.sz_ctas + q.copy_ctas + (p.n_runs ? t.t_tiles : 0)), 256, 0, st>>>(q);
   TB_LAUNCH_CHECK();
   TB_TRY(back ? packed_tc_backward(p, xmap, wmap, t.pairs, st) : packed_tc_forward(p, xmap, wmap, t.pairs, st));
   if (t.splits > 1) {
     const long long n4 = (long long)p.n_tok * p.n_cols / 4;
     const long long nb = (n4 + 255) / 256;
-    k_packed_join<<<(unsigned)(nb < 4096 ? nb : 4096), 256, 0, st>>>(reinterpret_cast<const float4*>(p.part), reinterpret_cast<uint2*>(out), n4, t.splits);
+    k_packed_join<<<(unsigned)(nb < 4096 ? nb : 4096), 256, 0, st>>>(reinterpret_cast<const float4*>(p.part), reinterpret_cast<uint2*>(out), n4,
+                                                                          p.n_cols / 4, t.splits, ad, low, p.M);
     TB_LAUNCH_CHECK();
   }
   return TB_OK;

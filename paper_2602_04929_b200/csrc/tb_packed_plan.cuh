@@ -26,7 +26,7 @@ struct PackedTc {
   const unsigned* words;   // the packed rows, `pitch` words apart (a multiple of 16 bytes)
   int rows_pad, pitch;
   const int4* runs;        // per token tile, from its first token's index on: first token, end, adapter
-  const int* n_runs;       // per token tile
+  const int* n_runs;       // per token tile; nullptr: no adapters, or added with the splits' sums
   __nv_bfloat16* out;      // [n_tok][n_cols]
   float* part;             // splits > 1: [split][n_tok][n_cols]
   int n_tok, n_cols, n_sum, n_tile, m_tiles, t_tiles, splits, split_len;

@@ -25,6 +25,7 @@
 #pragma once
 
 #include "tb_packed.cuh"
+#include "tb_packed_decode.cuh"
 #include "tb_packed_plan.cuh"
 #include "tb_pair.cuh"
 
@@ -62,61 +63,6 @@ struct Parts {
     end = min(group_end, end + part);
   }
 };
-
-// Field of NB bits from bit POS of the words on.
-template <int POS, int NB, int N>
-__device__ __forceinline__ unsigned field(const unsigned (&w)[N]) {
-  constexpr int i = POS >> 5, s = POS & 31;
-  unsigned v;
-  if constexpr (s + NB <= 32)
-    v = w[i] >> s;
-  else
-    v = __funnelshift_r(w[i], w[i + 1], s);
-  if constexpr (NB < 32) v &= (1u << NB) - 1u;
-  return v;
-}
-
-__device__ __forceinline__ unsigned bf2(__nv_bfloat162 v) { return *reinterpret_cast<const unsigned*>(&v); }
-__device__ __forceinline__ __nv_bfloat162 bf2(unsigned v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
-
-// A zero-point as the decoders take it, made once a call (k_packed_prep): -(128 + z) twice in bf16, or 2^23 + z in float for
-// eight bits.
-// Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
-// is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)
-// is joined with itself 16 - b bits higher.  Eight bits go through float.
-template <int BITS, int N>
-__device__ __forceinline__ unsigned apart(unsigned f) {  // f: N codes; a product where the two do not overlap, else an or
-  if constexpr (N * BITS <= 16 - BITS)
-    return f * (1u + (1u << (16 - BITS)));
-  else
-    return f | (f << (16 - BITS));
-}
-template <int BITS, int C0, int N>
-__device__ __forceinline__ void decode8(const unsigned (&w)[N], unsigned z, unsigned (&o)[4]) {
-  if constexpr (BITS == 8) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned v = w[(C0 + 2 * i) >> 2] >> (8 * ((C0 + 2 * i) & 3));
-      const float a = __uint_as_float(0x4B000000u | (v & 0xffu)) - __uint_as_float(z), b = __uint_as_float(0x4B000000u | ((v >> 8) & 0xffu)) - __uint_as_float(z);
-      o[i] = bf2(__floats2bfloat162_rn(a, b));
-    }
-  } else if constexpr (BITS <= 4) {
-    constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
-    const unsigned y0 = apart<BITS, 4>(field<C0 * BITS, 4 * BITS>(w)), y1 = apart<BITS, 4>(field<(C0 + 4) * BITS, 4 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
-    o[1] = bf2(__hadd2(bf2(((y0 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
-    o[2] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
-    o[3] = bf2(__hadd2(bf2(((y1 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
-  } else {
-    constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
-    const unsigned y0 = apart<BITS, 2>(field<C0 * BITS, 2 * BITS>(w)), y1 = apart<BITS, 2>(field<(C0 + 2) * BITS, 2 * BITS>(w));
-    const unsigned y2 = apart<BITS, 2>(field<(C0 + 4) * BITS, 2 * BITS>(w)), y3 = apart<BITS, 2>(field<(C0 + 6) * BITS, 2 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
-    o[1] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
-    o[2] = bf2(__hadd2(bf2((y2 & m) | 0x43004300u), bf2(z)));
-    o[3] = bf2(__hadd2(bf2((y3 & m) | 0x43004300u), bf2(z)));
-  }
-}
 
 // c - z, exact, times s, rounded to bf16 once
 __device__ __forceinline__ void scale8(unsigned (&o)[4], float s) {
@@ -255,7 +201,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
     r.t0 = ti * p.n_tile;
     r.k0 = r.split * p.split_len;
     r.k1 = min(p.n_sum, r.k0 + p.split_len);
-    r.n_runs = p.ad.n && r.split == 0 ? p.n_runs[ti] : 0;
+    r.n_runs = p.n_runs ? p.n_runs[ti] : 0;
     r.lora = (r.n_runs * nb * 2 + 3) >> 2;  // stages of four slots
     return r;
   };
@@ -472,13 +418,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           ++it;
         }
       }
-      // the adapters: four slots a stage, slot = (run, 16 of the rank, piece)
+      // the adapters (where the sum is not split): four slots a stage, slot = (run, 16 of the rank, piece)
       const int n_slots = c.n_runs * nb * 2;
       for (int st = 0; st < c.lora && ok; ++st, ++it) {
         if ((int)(it & 1u) != turn) continue;
         const int s = it % STAGES;
-        ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
-        if (!ok) break;
         const uint32_t sa = base + s * PT_STAGE_BYTES, sb = sa + PT_A_BYTES;
         {
           // A: contraction row kk of 64 x two halves of 64 columns
@@ -487,22 +431,25 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           const int run = slot / (2 * nb), q = slot - run * 2 * nb, r = (q >> 1) * 16 + (kk & 15);
           const __nv_bfloat16* m = nullptr;
           if (slot < n_slots && r < p.ad.rank) m = p.M + ((long long)p.runs[c.t0 + run].z * p.ad.rank + r) * p.n_cols;
-          bool odd = false;
+          uint4 v[8];
 #pragma unroll
           for (int ch = 0; ch < 8; ++ch) {
             const int col = c.m0 + 64 * hf + 8 * ch;
-            unsigned o[4] = {0u, 0u, 0u, 0u};
-            if (m && col < p.n_cols) {
-              const uint4 v = __ldg(reinterpret_cast<const uint4*>(m + col));
-              o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+            v[ch] = m && col < p.n_cols ? __ldg(reinterpret_cast<const uint4*>(m + col)) : make_uint4(0u, 0u, 0u, 0u);
+          }
+          ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
+          if (!ok) break;
+          bool odd = false;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (not_finite2(o[i])) {
-                  odd = true;
-                  if ((o[i] & 0x7f80u) == 0x7f80u) o[i] &= 0xffff0000u;
-                  if ((o[i] & 0x7f800000u) == 0x7f800000u) o[i] &= 0xffffu;
-                }
-            }
+          for (int ch = 0; ch < 8; ++ch) {
+            unsigned o[4] = {v[ch].x, v[ch].y, v[ch].z, v[ch].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (not_finite2(o[i])) {
+                odd = true;
+                if ((o[i] & 0x7f80u) == 0x7f80u) o[i] &= 0xffff0000u;
+                if ((o[i] & 0x7f800000u) == 0x7f800000u) o[i] &= 0xffffu;
+              }
             sts16(sa + (uint32_t)hf * 8192u + (uint32_t)kk * 128u + (((uint32_t)ch ^ (uint32_t)(kk & 7)) << 4), o);
           }
           if (odd) *odd_flag = 1;
@@ -609,12 +556,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
             const float m = __bfloat162float(p.M[((long long)ru.z * p.ad.rank + r) * p.n_cols + col]);
             if (fabsf(m) <= 3.4028234e38f) continue;
             for (int tok = max(ru.x, tok0); tok < min(ru.y, tok0 + n); ++tok) {
-              const float v = f * p.low[(long long)tok * p.ad.rank + r] * m;
               const long long i = (long long)(tok - tok0) * p.n_cols;
-              if (p.splits > 1)
-                fo[i] += v;
-              else
-                bo[i] = __float2bfloat16(__bfloat162float(bo[i]) + v);
+              bo[i] = __float2bfloat16(__bfloat162float(bo[i]) + f * p.low[(long long)tok * p.ad.rank + r] * m);
             }
           }
         }
