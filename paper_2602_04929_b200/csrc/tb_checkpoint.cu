@@ -4,8 +4,10 @@
 // 16-byte loads of float), so a run's maximum is four shuffles away and a warp stores 256 bytes of codes.  A lane has two
 // such pieces in flight.
 //
-// The codes are those of the true quotient: x * (1 / scale) lands within one of it, and the sign of x - (q +- 1/2) scale,
-// which one fused multiply-add gives exactly, says whether q is the nearest; a tie (the sum is 0) goes to the even one.
+// The codes are those of the true quotient.  y = x * (1 / scale) is off by less than 2^-14 where |y| <= 127, so rounding it decides
+// unless it lies that close to the middle between two codes.  Only a lane that has such a value looks further: the sign of x - (q +- 1/2) scale,
+// which one fused multiply-add gives exactly, says whether q is the nearest, and a tie (the sum is 0) goes to the even one.  Rounding
+// is one addition: 1.5 * 2^23 + y has the code in its low bits.
 #include "tb_packed.cuh"
 
 namespace tb {
@@ -53,21 +55,29 @@ __device__ __forceinline__ int nearest_code(float x, float s, float inv) {
   return (int)fminf(fmaxf(q, -127.0f), 127.0f);
 }
 
-// Units of 8 values, numbered token by token with every token's last run filled up to 16 units.
+constexpr int CKPT_PER = 2;  // runs that a lane has in flight
+
+// run -> token and column; per_inv: 2^64 / n_g rounded up, 0 for one run a token
+__device__ __forceinline__ void place_of(long long run, int n_g, unsigned long long per_inv, int l, long long& t, int& col) {
+  t = per_inv ? (long long)__umul64hi((unsigned long long)run, per_inv) : run;
+  col = (int)(run - t * n_g) * CKPT_RUN + 8 * l;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x, signed char* __restrict__ codes,
-                                                         float* __restrict__ scales, long long n_runs, int d, int n_g) {
+                                                         float* __restrict__ scales, long long n_runs, int d, int n_g,
+                                                         unsigned long long per_inv) {
   const int half = threadIdx.x >> 4, l = threadIdx.x & 15;
-  constexpr int PER = 2;
-  const long long r0 = (long long)blockIdx.x * (16 * PER) + half;
-  float v[PER][8];
-  bool in[PER];
-  long long at[PER];
+  const long long r0 = (long long)blockIdx.x * (16 * CKPT_PER) + half;
+  float v[CKPT_PER][8];
+  bool in[CKPT_PER];
+  long long at[CKPT_PER];
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
+  for (int k = 0; k < CKPT_PER; ++k) {
     const long long run = r0 + 16 * k;
-    const long long t = run / n_g;
-    const int col = (int)(run - t * n_g) * CKPT_RUN + 8 * l;
+    long long t;
+    int col;
+    place_of(run, n_g, per_inv, l, t, col);
     in[k] = run < n_runs && col < d;
     at[k] = t * d + col;
 #pragma unroll
@@ -75,7 +85,7 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
     if (in[k]) load8(x + at[k], v[k]);
   }
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
+  for (int k = 0; k < CKPT_PER; ++k) {
     unsigned top = 0;  // magnitudes as integers: they order like the values, and what is not finite comes out on top
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
@@ -83,17 +93,31 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
     for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool finite = top < 0x7f800000u;
     const float s = finite ? __fdiv_rn(__uint_as_float(top), 127.0f) : __uint_as_float(0x7fffffffu);
-    // a scale below 2^-126 has no float reciprocal worth the name: scaled up by 2^64 it has, and so has x
-    const bool tiny = s < 1.17549435e-38f;
-    const float up = tiny ? 18446744073709551616.0f : 1.0f;
-    const float su = s * up, inv = su > 0.0f ? 1.0f / su : 0.0f;
+    const float inv = __fdiv_rn(1.0f, s);
     unsigned w[2] = {0, 0};
-    if (finite && su > 0.0f) {
+    if (finite && s >= 1.17549435e-38f) {
+      constexpr float magic = 12582912.0f;
+      unsigned q[8];
+      float off = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const unsigned q = (unsigned)nearest_code(v[k][i] * up, su, inv) & 0xffu;
-        w[i >> 2] |= q << (8 * (i & 3));
+        const float y = v[k][i] * inv, r = y + magic;
+        q[i] = __float_as_uint(r);
+        off = fmaxf(off, fabsf(y - (r - magic)));
       }
+      if (off > 0.5f - 6.1035156e-5f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = (unsigned)nearest_code(v[k][i], s, inv);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        w[h] = __byte_perm(__byte_perm(q[4 * h], q[4 * h + 1], 0x0040), __byte_perm(q[4 * h + 2], q[4 * h + 3], 0x0040), 0x5410);
+    } else if (finite && s > 0.0f) {
+      // a scale below 2^-126 has no float reciprocal worth the name: scaled up by 2^64 it has, and so has x
+      constexpr float up = 18446744073709551616.0f;
+      const float su = s * up, iu = 1.0f / su;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i >> 2] |= ((unsigned)nearest_code(v[k][i] * up, su, iu) & 0xffu) << (8 * (i & 3));
     }
     if (in[k]) *reinterpret_cast<uint2*>(codes + at[k]) = make_uint2(w[0], w[1]);
     if (l == 0 && r0 + 16 * k < n_runs) scales[r0 + 16 * k] = s;
@@ -103,22 +127,30 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
 template <typename T>
 __global__ void __launch_bounds__(256) k_checkpoint_unpack(const signed char* __restrict__ codes,
                                                            const float* __restrict__ scales, T* __restrict__ x,
-                                                           long long n_runs, int d, int n_g) {
+                                                           long long n_runs, int d, int n_g, unsigned long long per_inv) {
   const int half = threadIdx.x >> 4, l = threadIdx.x & 15;
-  constexpr int PER = 2;
+  uint2 w[CKPT_PER];
+  float s[CKPT_PER];
+  long long at[CKPT_PER];
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const long long run = (long long)blockIdx.x * (16 * PER) + 16 * k + half;
-    const long long t = run / n_g;
-    const int col = (int)(run - t * n_g) * CKPT_RUN + 8 * l;
-    if (run >= n_runs || col >= d) continue;
-    const long long at = t * d + col;
-    const uint2 w = __ldcs(reinterpret_cast<const uint2*>(codes + at));
-    const float s = __ldg(scales + run);
+  for (int k = 0; k < CKPT_PER; ++k) {
+    const long long run = (long long)blockIdx.x * (16 * CKPT_PER) + 16 * k + half;
+    long long t;
+    int col;
+    place_of(run, n_g, per_inv, l, t, col);
+    at[k] = run < n_runs && col < d ? t * d + col : -1;
+    if (at[k] >= 0) {
+      w[k] = __ldcs(reinterpret_cast<const uint2*>(codes + at[k]));
+      s[k] = __ldg(scales + run);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < CKPT_PER; ++k) {
+    if (at[k] < 0) continue;
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(signed char)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
-    store8(x + at, v);
+    for (int i = 0; i < 8; ++i) v[i] = (float)(signed char)((i < 4 ? w[k].x : w[k].y) >> (8 * (i & 3))) * s[k];
+    store8(x + at[k], v);
   }
 }
 
@@ -127,11 +159,13 @@ __global__ void __launch_bounds__(256) k_checkpoint_unpack(const signed char* __
 using namespace tb;
 
 static tb_status checkpoint_shape(tb_dtype type, long long n_tok, int d, const void* x, const void* codes,
-                                  const void* scales, long long* n_runs, unsigned* blocks) {
+                                  const void* scales, long long* n_runs, unsigned* blocks, unsigned long long* per_inv) {
   if ((type != TB_F32 && type != TB_BF16) || n_tok < 0 || d <= 0) return TB_ERR_INVALID_ARG;
   if (d % 32) return TB_ERR_UNSUPPORTED;
   *n_runs = n_tok * ((d + CKPT_RUN - 1) / CKPT_RUN);
-  const long long nb = (*n_runs + 31) / 32;
+  const unsigned long long n_g = (unsigned)(d + CKPT_RUN - 1) / CKPT_RUN;
+  *per_inv = n_g > 1 ? ~0ull / n_g + 1 : 0;
+  const long long nb = (*n_runs + 16 * CKPT_PER - 1) / (16 * CKPT_PER);
   if (n_tok > 0x7fffffffll || nb > 0x7fffffffll) return TB_ERR_UNSUPPORTED;
   *blocks = (unsigned)nb;
   if (n_tok == 0) return TB_OK;
@@ -144,13 +178,14 @@ extern "C" tb_status tb_checkpoint_pack(const void* x, tb_dtype x_type, long lon
                                         float* scales, void* stream) {
   long long n_runs;
   unsigned nb;
-  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb));
+  unsigned long long per_inv;
+  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb, &per_inv));
   if (nb == 0) return TB_OK;
   const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
   if (x_type == TB_BF16)
-    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const __nv_bfloat16*>(x), codes, scales, n_runs, d, n_g);
+    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const __nv_bfloat16*>(x), codes, scales, n_runs, d, n_g, per_inv);
   else
-    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const float*>(x), codes, scales, n_runs, d, n_g);
+    k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const float*>(x), codes, scales, n_runs, d, n_g, per_inv);
   TB_LAUNCH_CHECK();
   return TB_OK;
 }
@@ -159,13 +194,14 @@ extern "C" tb_status tb_checkpoint_unpack(const signed char* codes, const float*
                                           tb_dtype x_type, void* x, void* stream) {
   long long n_runs;
   unsigned nb;
-  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb));
+  unsigned long long per_inv;
+  TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb, &per_inv));
   if (nb == 0) return TB_OK;
   const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
   if (x_type == TB_BF16)
-    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<__nv_bfloat16*>(x), n_runs, d, n_g);
+    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<__nv_bfloat16*>(x), n_runs, d, n_g, per_inv);
   else
-    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<float*>(x), n_runs, d, n_g);
+    k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<float*>(x), n_runs, d, n_g, per_inv);
   TB_LAUNCH_CHECK();
   return TB_OK;
 }

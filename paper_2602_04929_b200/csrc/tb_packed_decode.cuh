@@ -21,10 +21,20 @@ __device__ __forceinline__ unsigned field(const unsigned (&w)[N]) {
 __device__ __forceinline__ unsigned bf2(__nv_bfloat162 v) { return *reinterpret_cast<const unsigned*>(&v); }
 __device__ __forceinline__ __nv_bfloat162 bf2(unsigned v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
 
+// (v & mask) | bits in one instruction: with two constants the compiler makes two of it
+__device__ __forceinline__ unsigned masked(unsigned v, unsigned mask, unsigned bits) {
+  unsigned o;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(o) : "r"(v), "r"(mask), "r"(bits));
+  return o;
+}
+// small integers to float without the conversion unit
+__device__ __forceinline__ float small_float(int v) { return __int_as_float(0x4B400000 + v) - 12582912.0f; }
+
 // A zero-point as the decoders take it: -(128 + z) twice in bf16, or 2^23 + z in float for eight bits.
 __device__ __forceinline__ unsigned zero_word(int z, int bits) {
   if (bits == 8) return __float_as_uint((float)(8388608 + z));
-  return bf2(__float2bfloat162_rn((float)(-128 - z)));
+  z = max(-4000000, min(4000000, z));  // far beyond what eight bits keep apart
+  return bf2(__float2bfloat162_rn(-128.0f - small_float(z)));
 }
 // Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
 // is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)
@@ -48,18 +58,18 @@ __device__ __forceinline__ void decode8(const unsigned (&w)[N], unsigned z, unsi
   } else if constexpr (BITS <= 4) {
     constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
     const unsigned y0 = apart<BITS, 4>(field<C0 * BITS, 4 * BITS>(w)), y1 = apart<BITS, 4>(field<(C0 + 4) * BITS, 4 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
-    o[1] = bf2(__hadd2(bf2(((y0 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
-    o[2] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
-    o[3] = bf2(__hadd2(bf2(((y1 >> (2 * BITS)) & m) | 0x43004300u), bf2(z)));
+    o[0] = bf2(__hadd2(bf2(masked(y0, m, 0x43004300u)), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(masked((y0 >> (2 * BITS)), m, 0x43004300u)), bf2(z)));
+    o[2] = bf2(__hadd2(bf2(masked(y1, m, 0x43004300u)), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(masked((y1 >> (2 * BITS)), m, 0x43004300u)), bf2(z)));
   } else {
     constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
     const unsigned y0 = apart<BITS, 2>(field<C0 * BITS, 2 * BITS>(w)), y1 = apart<BITS, 2>(field<(C0 + 2) * BITS, 2 * BITS>(w));
     const unsigned y2 = apart<BITS, 2>(field<(C0 + 4) * BITS, 2 * BITS>(w)), y3 = apart<BITS, 2>(field<(C0 + 6) * BITS, 2 * BITS>(w));
-    o[0] = bf2(__hadd2(bf2((y0 & m) | 0x43004300u), bf2(z)));
-    o[1] = bf2(__hadd2(bf2((y1 & m) | 0x43004300u), bf2(z)));
-    o[2] = bf2(__hadd2(bf2((y2 & m) | 0x43004300u), bf2(z)));
-    o[3] = bf2(__hadd2(bf2((y3 & m) | 0x43004300u), bf2(z)));
+    o[0] = bf2(__hadd2(bf2(masked(y0, m, 0x43004300u)), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(masked(y1, m, 0x43004300u)), bf2(z)));
+    o[2] = bf2(__hadd2(bf2(masked(y2, m, 0x43004300u)), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(masked(y3, m, 0x43004300u)), bf2(z)));
   }
 }
 

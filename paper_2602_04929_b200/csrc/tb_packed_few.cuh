@@ -1,13 +1,18 @@
 // y = x Q^T for a few tokens (bf16), and for any number of them in float: mma.sync on weights decoded in registers.
 //
-// With few tokens the product is bound by reading the packed words and, at two to four bits, nearly as much by the
-// instructions that decode them, so the words go from global memory straight into fragments.  A weight row is a row of operand A
-// (16 rows a tile, MT tiles a CTA), tokens are operand B's columns (NT tiles of 8).  Which contraction columns a fragment calls
-// k = 0 .. 15 does not matter as long as both operands agree: a lane takes 32 neighbouring codes of a row (BITS words), hence its
-// quad 128 columns, and the same columns of x; eight codes decode to the four registers that two MMAs take.  c - z is exact in
-// bf16; the scale of a row and of the 128 columns multiplies the sum.  The CTA's warps take every eighth block of 128 columns, the
-// CTAs of a cluster (cs of them) every cs-th eight; sums are joined in a fixed order.  Float activations go through three bf16 pieces, all
-// 24 bits.
+// With few tokens the product is bound by reading the packed words and, at two to four bits, as much by the instructions that
+// decode them (logical operations go at half rate), so the words are
+// decoded straight into fragments.  A weight row is a
+// row of operand A (16 rows a tile, MT tiles a CTA), tokens are operand B's columns (NT tiles of 8).  Which contraction columns a
+// fragment calls k = 0 .. 15 does not matter as long as both operands agree: a lane takes 32 neighbouring codes of a row (BITS
+// words), hence its quad 128 columns, and the same columns of x; 16 codes decode to the eight registers that four MMAs take.  With
+// two and four bits a pair of neighbours in a register is a code of a word's lower half and the one 16 bits above it, so that a
+// mask extracts both, and it is x that is brought into that order, once for all MT tiles.  c - z is exact in bf16; the scale of a
+// row and of the 128 columns multiplies the sum.  Float activations go through three bf16 pieces, all 24 bits.
+//
+// The words come by bulk copies, a row's piece each, in stages of eight blocks of 128 columns (one for every warp), as many stages
+// ahead as fit beside a second CTA: a warp that loads its own words has too few bytes in flight for the memory's latency.  CTAs of a
+// cluster (cs of them) have a range of blocks each; the warps' and the CTAs' sums are joined in a fixed order.
 //
 // NARROW: scales of fewer than 128 columns, or a width that is no multiple of 128.  A lane then takes 8 codes of a run of 32.
 #pragma once
@@ -18,13 +23,16 @@
 
 namespace tb {
 
+enum { FEW_STAGES_MAX = 8 };
+static __device__ int g_few_error = 0;  // of this translation unit; tb_device_error_flag reads and clears all of them
+
 struct PackedFew {
   PackedW w;
   Adapt ad;
   const void *x, *M;  // M: the adapters' [adapter][rank][d_out]
   const float* low;   // [n_tok][rank]
   void* out;
-  int n_tok;
+  int n_tok, stages;
 };
 
 __device__ __forceinline__ void mma_few(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
@@ -74,8 +82,98 @@ __device__ __forceinline__ void few_step(const unsigned (&w0)[N], const unsigned
     }
 }
 
+// Columns of register i of 16: the lower half's, the upper half's.
 template <int BITS>
-__device__ __forceinline__ void load_words(const unsigned* p, unsigned (&w)[BITS]) {  // on a multiple of BITS words
+struct Pair {
+  static __host__ __device__ constexpr int lo(int i) { return BITS == 2 ? i : BITS == 4 ? (i & 3) + 8 * (i >> 2) : 2 * i; }
+  static __host__ __device__ constexpr int hi(int i) { return lo(i) + (BITS == 2 ? 8 : BITS == 4 ? 4 : 1); }
+};
+template <int NP>
+struct Acts16 {
+  unsigned v[NP][8];
+};
+// 16 neighbouring activations as they are loaded, and as pieces of bf16 pairs.
+template <int NP>
+struct Raw16 {
+  uint4 v[NP == 1 ? 2 : 4];
+  template <typename T>
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (NP == 1 ? 2 : 4); ++i) v[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+};
+template <int BITS>
+__device__ __forceinline__ void pieces16(const Raw16<1>& x, Acts16<1>& a) {
+  const unsigned r[8] = {x.v[0].x, x.v[0].y, x.v[0].z, x.v[0].w, x.v[1].x, x.v[1].y, x.v[1].z, x.v[1].w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (BITS == 2 || BITS == 4)
+      a.v[0][i] = __byte_perm(r[Pair<BITS>::lo(i) >> 1], r[Pair<BITS>::hi(i) >> 1], i & 1 ? 0x7632 : 0x5410);
+    else
+      a.v[0][i] = r[i];
+  }
+}
+template <int BITS>
+__device__ __forceinline__ void pieces16(const Raw16<3>& x, Acts16<3>& a) {
+  float f[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[4 * i] = __uint_as_float(x.v[i].x), f[4 * i + 1] = __uint_as_float(x.v[i].y);
+    f[4 * i + 2] = __uint_as_float(x.v[i].z), f[4 * i + 3] = __uint_as_float(x.v[i].w);
+  }
+#pragma unroll
+  for (int n = 0; n < 3; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float &fl = f[Pair<BITS>::lo(i)], &fh = f[Pair<BITS>::hi(i)];
+      a.v[n][i] = bf2(__floats2bfloat162_rn(fl, fh));
+      const float lo = __uint_as_float(a.v[n][i] << 16), hi = __uint_as_float(a.v[n][i] & 0xffff0000u);
+      fl = fabsf(lo) <= 3.3895e38f ? fl - lo : 0.0f;
+      fh = fabsf(hi) <= 3.3895e38f ? fh - hi : 0.0f;
+    }
+}
+
+// Codes 16 H .. 16 H + 15 of a lane's words, in that order.  A code p bits up in the mantissa of 2^(7 - p) is 2^(7 - p) + c.
+template <int BITS, int H>
+__device__ __forceinline__ void decode16(const unsigned (&w)[BITS], unsigned z, unsigned (&o)[8]) {
+  if constexpr (BITS == 2) {
+    const __nv_bfloat162 z0 = bf2(z), z2 = __hadd2(z0, __float2bfloat162_rn(96.0f)), z4 = __hadd2(z0, __float2bfloat162_rn(120.0f));
+    unsigned v = w[H];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i == 3 || i == 6) v >>= 6;
+      if (i % 3 == 0) o[i] = bf2(__hadd2(bf2(masked(v, 0x00030003u, 0x43004300u)), z0));
+      if (i % 3 == 1) o[i] = bf2(__hadd2(bf2(masked(v, 0x000c000cu, 0x42004200u)), z2));
+      if (i % 3 == 2) o[i] = bf2(__hadd2(bf2(masked(v, 0x00300030u, 0x41004100u)), z4));
+    }
+  } else if constexpr (BITS == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = bf2(__hadd2(bf2(masked(w[2 * H + (i >> 2)] >> (4 * (i & 3)), 0x000f000fu, 0x43004300u)), bf2(z)));
+  } else {
+    unsigned a[4], b[4];
+    decode8<BITS, 16 * H>(w, z, a);
+    decode8<BITS, 16 * H + 8>(w, z, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = a[i], o[4 + i] = b[i];
+  }
+}
+template <int BITS, int H, int NT, int NP>
+__device__ __forceinline__ void few_step16(const unsigned (&w0)[BITS], const unsigned (&w1)[BITS], unsigned z0, unsigned z1,
+                                           const Acts16<NP> (&x)[NT], float (&acc)[NT][4]) {
+  unsigned a[8], b[8];
+  decode16<BITS, H>(w0, z0, a);
+  decode16<BITS, H>(w1, z1, b);
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) mma_few(acc[n], a[i], b[i], a[i + 1], b[i + 1], x[n].v[p][i], x[n].v[p][i + 1]);
+}
+
+template <int BITS>
+__device__ __forceinline__ void load_words(const unsigned char* at, unsigned (&w)[BITS]) {  // shared memory, on a multiple of 4 BITS bytes
+  const unsigned* p = reinterpret_cast<const unsigned*>(at);
   if constexpr (BITS % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < BITS / 4; ++i) {
@@ -95,64 +193,100 @@ __device__ __forceinline__ void load_words(const unsigned* p, unsigned (&w)[BITS
 }
 
 template <int BITS, int MT, int NT, int NP, bool NARROW, typename T>
-__global__ void __launch_bounds__(256, 2) k_packed_few(const PackedFew p) {
+__global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const __grid_constant__ PackedFew p) {
   constexpr int RC = 16 * MT, TB = 8 * NT, OUT = RC * TB;
-  extern __shared__ float few_part[];  // [8 warps][token][row]
+  extern __shared__ __align__(128) float few_part[];  // a ring of the words' stages, then [8 warps][token][row]
   __shared__ int own[TB];
+  __shared__ __align__(8) unsigned long long bars[FEW_STAGES_MAX];
+  __shared__ int gave_up;
+  if (!NARROW && threadIdx.x == 0) {
+    for (int s = 0; s < FEW_STAGES_MAX; ++s) mbar_init(smem_u32(bars + s), 1);
+    gave_up = 0;
+    mbar_fence_init();
+  }
+  __syncthreads();
   uint32_t rank, cs;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int r0 = (blockIdx.x / cs) * RC, t0 = blockIdx.y * TB;
   if (p.ad.n && threadIdx.x < TB) own[threadIdx.x] = t0 + (int)threadIdx.x < p.n_tok ? adapter_of(p.ad, t0 + threadIdx.x) : -1;
-  const unsigned* row[2 * MT];
-  long long sz[2 * MT];
-#pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    const int r = min(r0 + 8 * i + g, p.w.d_out - 1);  // rows behind the last are computed from it and not stored
-    row[i] = p.w.packed + (long long)r * p.w.words;
-    sz[i] = (long long)r * p.w.n_g;
-  }
+  // rows come eight at a time, d_out is a multiple of eight: those behind the last are taken to be the last eight and not stored
+  const int eights = min(2 * MT, (p.w.d_out - r0) >> 3) - 1;
+  const unsigned* row0 = p.w.packed + (long long)(r0 + g) * p.w.words;
+  const long long sz0 = (long long)(r0 + g) * p.w.n_g;
   const T* x[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) x[n] = static_cast<const T*>(p.x) + (long long)min(t0 + 8 * n + g, p.n_tok - 1) * p.w.d_in;
   float sum[MT][NT][4] = {};
   if constexpr (!NARROW) {
+    constexpr int PITCH = 9 * 16 * BITS, STAGE = RC * PITCH;  // eight blocks of a row, and one to spread the rows over the banks
     const int blocks = p.w.d_in >> 7, per_group = p.w.group >> 7;
-#pragma unroll 1
-    for (int b = (int)rank * 8 + warp; b < blocks; b += 8 * (int)cs) {
-      unsigned w[2 * MT][BITS];
-      int z[2 * MT];
-      float s[2 * MT];
-      const int gi = b / per_group;
-#pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) {
-        load_words<BITS>(row[i] + (4 * b + q) * BITS, w[i]);
-        z[i] = p.w.zeros[sz[i] + gi];
-        s[i] = p.w.scales[sz[i] + gi];
+    const int per = (blocks + (int)cs - 1) / (int)cs, b0 = (int)rank * per, b_end = min(blocks, b0 + per);
+    const int n_st = b_end > b0 ? (b_end - b0 + 7) >> 3 : 0;
+    unsigned char* ring = reinterpret_cast<unsigned char*>(few_part);
+    const uint32_t ring0 = smem_u32(few_part), bar0 = smem_u32(bars);
+    auto fill = [&](int st) {  // by all threads: one row each
+      const int s = st % p.stages, n = min(8, b_end - b0 - 8 * st);
+      if (threadIdx.x == 0) mbar_expect_tx(bar0 + 8 * s, RC * n * 16 * BITS);
+      __syncwarp();
+      if (threadIdx.x < RC) {
+        const long long r = min(r0 + (int)threadIdx.x, p.w.d_out - 1);
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                         ring0 + s * STAGE + threadIdx.x * PITCH),
+                     "l"(p.w.packed + r * p.w.words + (long long)(b0 + 8 * st) * 4 * BITS), "r"(n * 16 * BITS), "r"(bar0 + 8 * s)
+                     : "memory");
       }
-      float acc[MT][NT][4] = {};
+    };
+    for (int st = 0; st < min(n_st, p.stages); ++st) fill(st);
+#pragma unroll 1
+    for (int st = 0; st < n_st; ++st) {
+      const int s = st % p.stages, b = b0 + 8 * st + warp;
+      const bool mine = b < b_end;
+      int z[2 * MT];
+      float sc[2 * MT];
+      Raw16<NP> raw[2][NT];
+      if (mine) {
+        const long long gi = sz0 + b / per_group;
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) z[i] = (int)zero_word(z[i], BITS);
-#define TB_FEW_STEP(C)                                                                                                 \
-  {                                                                                                                    \
-    Acts<NP> a[NT];                                                                                                    \
-    _Pragma("unroll") for (int n = 0; n < NT; ++n) load_acts(x[n] + 128 * b + 32 * q + 8 * C, a[n]);                    \
-    _Pragma("unroll") for (int m = 0; m < MT; ++m)                                                                      \
-        few_step<BITS, C, NT, NP>(w[2 * m], w[2 * m + 1], (unsigned)z[2 * m], (unsigned)z[2 * m + 1], a, acc[m]);       \
-  }
-      TB_FEW_STEP(0)
-      TB_FEW_STEP(1)
-      TB_FEW_STEP(2)
-      TB_FEW_STEP(3)
-#undef TB_FEW_STEP
+        for (int i = 0; i < 2 * MT; ++i) {
+          const long long e = gi + (long long)(8 * min(i, eights)) * p.w.n_g;
+          z[i] = p.w.zeros[e], sc[i] = p.w.scales[e];
+        }
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n) raw[h][n].load(x[n] + 128 * b + 32 * q + 16 * h);
+      }
+      const bool landed = __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * s, (st / p.stages) & 1u, &gave_up, &g_few_error));
+      if (mine && landed) {  // (a wait that gave up leaves its share out; nobody skips a barrier)
+        Acts16<NP> a[2][NT];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) sum[m][n][c] = fmaf(s[2 * m + (c >> 1)], acc[m][n][c], sum[m][n][c]);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) pieces16<BITS>(raw[h][n], a[h][n]);
+        const unsigned char* at = ring + s * STAGE + g * PITCH + (4 * warp + q) * 4 * BITS;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          unsigned w0[BITS], w1[BITS];
+          load_words<BITS>(at + 16 * m * PITCH, w0);
+          load_words<BITS>(at + (16 * m + 8) * PITCH, w1);
+          const unsigned z0 = zero_word(z[2 * m], BITS), z1 = zero_word(z[2 * m + 1], BITS);
+          float acc[NT][4] = {};
+          few_step16<BITS, 0, NT, NP>(w0, w1, z0, z1, a[0], acc);
+          few_step16<BITS, 1, NT, NP>(w0, w1, z0, z1, a[1], acc);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[m][n][c] = fmaf(sc[2 * m + (c >> 1)], acc[n][c], sum[m][n][c]);
+        }
+      }
+      if (st + p.stages < n_st) {
+        __syncthreads();
+        fill(st + p.stages);
+      }
     }
+    __syncthreads();  // the ring becomes the sums'
   } else {
     const int runs = p.w.d_in >> 5, per_group = p.w.group >> 5;
 #pragma unroll 1
@@ -169,12 +303,13 @@ __global__ void __launch_bounds__(256, 2) k_packed_few(const PackedFew p) {
         float s[2], acc[NT][4] = {};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const unsigned* v = row[2 * m + i] + b * BITS;
+          const long long e = 8 * min(2 * m + i, eights);
+          const unsigned* v = row0 + e * p.w.words + b * BITS;
           const unsigned v0 = v[first], v1 = v[min(first + 1, BITS - 1)];
           w[i][0] = __funnelshift_r(v0, v1, shift);
           w[i][1] = BITS > 4 ? __funnelshift_r(v1, v[min(first + 2, BITS - 1)], shift) : 0u;
-          z[i] = zero_word(p.w.zeros[sz[2 * m + i] + gi], BITS);
-          s[i] = p.w.scales[sz[2 * m + i] + gi];
+          z[i] = zero_word(p.w.zeros[sz0 + e * p.w.n_g + gi], BITS);
+          s[i] = p.w.scales[sz0 + e * p.w.n_g + gi];
         }
         few_step<BITS, 0, NT, NP>(w[0], w[1], z[0], z[1], a, acc);
 #pragma unroll
@@ -232,21 +367,27 @@ __global__ void __launch_bounds__(256, 2) k_packed_few(const PackedFew p) {
 }
 
 template <int BITS, int NT, int NP, bool NARROW, typename T>
-tb_status launch_few(const PackedFew& p, cudaStream_t st) {
-  constexpr int MT = BITS <= 4 && NP * NT <= 3 ? 4 : 2, RC = 16 * MT, smem = 8 * RC * 8 * NT * 4;  // what 128 registers hold
+tb_status launch_few(PackedFew p, cudaStream_t st) {
+  constexpr int MT = BITS <= 4 && NP * NT <= 3 ? 4 : 2, RC = 16 * MT;  // what 128 registers hold
+  constexpr int sums = 8 * RC * 8 * NT * 4, stage = NARROW ? 1 : RC * 9 * 16 * BITS, room = NT * NP == 1 ? 110 * 1024 : 220 * 1024;
   auto kern = k_packed_few<BITS, MT, NT, NP, NARROW, T>;
   static bool configured[64] = {false};
   int dev = 0;
   TB_CUDA_CHECK(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return TB_ERR_CUDA;
   if (!configured[dev]) {
-    TB_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    TB_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, room));
     configured[dev] = true;
   }
   const int tiles = (p.w.d_out + RC - 1) / RC, blocks = (p.n_tok + 8 * NT - 1) / (8 * NT);
   const int sms = sm_count() > 0 ? sm_count() : 148, units = p.w.d_in >> (NARROW ? 5 : 7);
   int cs = 1;  // CTAs along the contraction, up to two an SM, a block of columns for every warp
   while (cs < 8 && (long long)tiles * blocks * cs * 2 <= 2 * sms && 8 * cs < units) cs *= 2;
+  // all of a CTA's stages at once where they fit
+  const int n_st = ((units + cs - 1) / cs + 7) / 8, fit = room / stage;
+  p.stages = NARROW ? 1 : n_st < fit ? n_st : fit;
+  if (p.stages > FEW_STAGES_MAX) p.stages = FEW_STAGES_MAX;
+  const int smem = NARROW || p.stages * stage < sums ? sums : p.stages * stage;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * cs), (unsigned)blocks);
   cfg.blockDim = dim3(256);
@@ -278,6 +419,16 @@ tb_status launch_few_bits(const PackedFew& p, cudaStream_t st) {
     case 7: return narrow ? launch_few<7, NT, NP, true, T>(p, st) : launch_few<7, NT, NP, false, T>(p, st);
     default: return narrow ? launch_few<8, NT, NP, true, T>(p, st) : launch_few<8, NT, NP, false, T>(p, st);
   }
+}
+
+static int few_tu_error_read_clear() {
+  int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_few_error, sizeof(int)) != cudaSuccess) return -1;
+  if (v) {
+    int z = 0;
+    cudaMemcpyToSymbol(g_few_error, &z, sizeof(int));
+  }
+  return v;
 }
 
 }  // namespace tb

@@ -4,5 +4,6 @@
 namespace tb {
 
 tb_status packed_few_bf16_1(const PackedFew& p, cudaStream_t st) { return launch_few_bits<1, 1, __nv_bfloat16>(p, st); }
+int packed_few_bf16_1_error_read_clear() { return few_tu_error_read_clear(); }
 
 }  // namespace tb

@@ -255,7 +255,11 @@ int sweep_error_read_clear();  // the same word of the column-sweep kernel (tb_s
 int yw_error_read_clear();     // and of the tensor-core product of the scale refinement (tb_gemm_tc.cu)
 int cross_error_read_clear();  // and of the deviation correlation (tb_cross_tc.cu)
 int packed_fwd_error_read_clear();  // the products with bit-packed weights (tb_packed_tc_fwd.cu,
-int packed_bwd_error_read_clear();  // tb_packed_tc_bwd.cu)
+int packed_bwd_error_read_clear();  // tb_packed_tc_bwd.cu,
+int packed_few_bf16_1_error_read_clear();  // tb_packed_few_*.cu)
+int packed_few_bf16_2_error_read_clear();
+int packed_few_f32_1_error_read_clear();
+int packed_few_f32_2_error_read_clear();
 int pair_error_read_clear();   // and of the CTA-pair form of the Hessian kernel (tb_syrk_tc2.cu)
 }
 
@@ -301,6 +305,12 @@ extern "C" int tb_device_error_flag(void) {
   const int q = tb::pair_error_read_clear();
   const int pf = tb::packed_fwd_error_read_clear();
   const int pb = tb::packed_bwd_error_read_clear();
+  const int few[4] = {tb::packed_few_bf16_1_error_read_clear(), tb::packed_few_bf16_2_error_read_clear(),
+                      tb::packed_few_f32_1_error_read_clear(), tb::packed_few_f32_2_error_read_clear()};
+  for (int i = 0; i < 4; ++i) {
+    if (few[i] < 0) return -1;
+    v |= few[i];
+  }
   if (e < 0 || c < 0 || g < 0 || w < 0 || y < 0 || x < 0 || q < 0 || pf < 0 || pb < 0) return -1;
   return (v || e || c || g || w || y || x || q || pf || pb) ? 1 : 0;
 }
