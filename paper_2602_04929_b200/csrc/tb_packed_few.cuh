@@ -10,9 +10,10 @@
 // mask extracts both, and it is x that is brought into that order, once for all MT tiles.  c - z is exact in bf16; the scale of a
 // row and of the 128 columns multiplies the sum.  Float activations go through three bf16 pieces, all 24 bits.
 //
-// The words come by bulk copies, a row's piece each, in stages of eight blocks of 128 columns (one for every warp), as many stages
-// ahead as fit beside a second CTA: a warp that loads its own words has too few bytes in flight for the memory's latency.  CTAs of a
-// cluster (cs of them) have a range of blocks each; the warps' and the CTAs' sums are joined in a fixed order.
+// The words come by TMA, in stages of eight blocks of 128 columns (one for every warp), as many stages ahead as fit beside a second
+// CTA: a warp that loads its own words has too few bytes in flight for the memory's latency.  A tile has the most rows (16 MT) that
+// leave a CTA and a half for every SM; where even 16 rows do not, CTAs of a cluster (cs of them) have a range of blocks each.  The
+// warps' and the CTAs' sums are joined in a fixed order.
 //
 // NARROW: scales of fewer than 128 columns, or a width that is no multiple of 128.  A lane then takes 8 codes of a run of 32.
 #pragma once
@@ -171,29 +172,28 @@ __device__ __forceinline__ void few_step16(const unsigned (&w0)[BITS], const uns
       for (int i = 0; i < 8; i += 2) mma_few(acc[n], a[i], b[i], a[i + 1], b[i + 1], x[n].v[p][i], x[n].v[p][i + 1]);
 }
 
-template <int BITS>
-__device__ __forceinline__ void load_words(const unsigned char* at, unsigned (&w)[BITS]) {  // shared memory, on a multiple of 4 BITS bytes
-  const unsigned* p = reinterpret_cast<const unsigned*>(at);
-  if constexpr (BITS % 4 == 0) {
+// A stage: 128-byte pieces of all rows, one after the other, in TMA's 128-byte swizzle.  A lane's BITS words from byte `at` of row r on.
+template <int BITS, int RC>
+__device__ __forceinline__ void load_words(const unsigned char* stage, int r, int at, unsigned (&w)[BITS]) {
+  constexpr int STEP = BITS % 4 == 0 ? 4 : BITS % 2 == 0 ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < BITS / 4; ++i) {
-      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  for (int i = 0; i < BITS; i += STEP) {
+    const int b = at + 4 * i;
+    const unsigned char* p = stage + (b >> 7) * (RC * 128) + r * 128 + (((((b & 127) >> 4) ^ (r & 7)) << 4) | (b & 15));
+    if constexpr (STEP == 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    } else if constexpr (STEP == 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[i] = v.x, w[i + 1] = v.y;
+    } else {
+      w[i] = *reinterpret_cast<const unsigned*>(p);
     }
-  } else if constexpr (BITS % 2 == 0) {
-#pragma unroll
-    for (int i = 0; i < BITS / 2; ++i) {
-      const uint2 v = reinterpret_cast<const uint2*>(p)[i];
-      w[2 * i] = v.x, w[2 * i + 1] = v.y;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < BITS; ++i) w[i] = p[i];
   }
 }
 
 template <int BITS, int MT, int NT, int NP, bool NARROW, typename T>
-__global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const __grid_constant__ PackedFew p) {
+__global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const __grid_constant__ PackedFew p, const __grid_constant__ CUtensorMap wmap) {
   constexpr int RC = 16 * MT, TB = 8 * NT, OUT = RC * TB;
   extern __shared__ __align__(128) float few_part[];  // a ring of the words' stages, then [8 warps][token][row]
   __shared__ int own[TB];
@@ -220,61 +220,72 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
   for (int n = 0; n < NT; ++n) x[n] = static_cast<const T*>(p.x) + (long long)min(t0 + 8 * n + g, p.n_tok - 1) * p.w.d_in;
   float sum[MT][NT][4] = {};
   if constexpr (!NARROW) {
-    constexpr int PITCH = 9 * 16 * BITS, STAGE = RC * PITCH;  // eight blocks of a row, and one to spread the rows over the banks
+    constexpr int STAGE = RC * 128 * BITS;  // eight blocks of 16 BITS bytes a row: BITS pieces
     const int blocks = p.w.d_in >> 7, per_group = p.w.group >> 7;
     const int per = (blocks + (int)cs - 1) / (int)cs, b0 = (int)rank * per, b_end = min(blocks, b0 + per);
     const int n_st = b_end > b0 ? (b_end - b0 + 7) >> 3 : 0;
-    unsigned char* ring = reinterpret_cast<unsigned char*>(few_part);
-    const uint32_t ring0 = smem_u32(few_part), bar0 = smem_u32(bars);
-    auto fill = [&](int st) {  // by all threads: one row each
-      const int s = st % p.stages, n = min(8, b_end - b0 - 8 * st);
-      if (threadIdx.x == 0) mbar_expect_tx(bar0 + 8 * s, RC * n * 16 * BITS);
-      __syncwarp();
-      if (threadIdx.x < RC) {
-        const long long r = min(r0 + (int)threadIdx.x, p.w.d_out - 1);
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                         ring0 + s * STAGE + threadIdx.x * PITCH),
-                     "l"(p.w.packed + r * p.w.words + (long long)(b0 + 8 * st) * 4 * BITS), "r"(n * 16 * BITS), "r"(bar0 + 8 * s)
-                     : "memory");
-      }
+    // the dynamic part starts on a multiple of 1024 in the swizzle's eyes
+    const uint32_t ring0 = (smem_u32(few_part) + 1023u) & ~1023u, bar0 = smem_u32(bars);
+    const unsigned char* ring = reinterpret_cast<const unsigned char*>(few_part) + (ring0 - smem_u32(few_part));
+    auto fill = [&](int st) {  // by one thread; what lies behind the columns or rows comes as zeros
+      const int s = st % p.stages;
+      mbar_expect_tx(bar0 + 8 * s, STAGE);
+      for (int k = 0; k < BITS; ++k)
+        tma_load_2d(ring0 + s * STAGE + k * (RC * 128), &wmap, (b0 + 8 * st) * 4 * BITS + 32 * k, r0, bar0 + 8 * s);
     };
-    for (int st = 0; st < min(n_st, p.stages); ++st) fill(st);
+    if (threadIdx.x == 0)
+      for (int st = 0; st < min(n_st, p.stages); ++st) fill(st);
+    // what a warp loads itself for a block, an iteration ahead: activations, zero-points, scales
+    struct Own {
+      Raw16<NP> x[2][NT];
+      int z[2 * MT];
+      float s[2 * MT];
+    } next;
+    const int* zeros = p.w.zeros + sz0;
+    const float* scales = p.w.scales + sz0;
+    auto fetch = [&](int b) {
+      const int gi = per_group == 1 ? b : b / per_group;
+#pragma unroll
+      for (int i = 0; i < 2 * MT; ++i) {
+        const int e = gi + 8 * min(i, eights) * p.w.n_g;
+        next.z[i] = zeros[e], next.s[i] = scales[e];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) next.x[h][n].load(x[n] + 128 * b + 32 * q + 16 * h);
+    };
+    if (b0 + warp < b_end) fetch(b0 + warp);
+    int s = 0;
+    uint32_t phase = 0;
 #pragma unroll 1
     for (int st = 0; st < n_st; ++st) {
-      const int s = st % p.stages, b = b0 + 8 * st + warp;
+      const int b = b0 + 8 * st + warp;
       const bool mine = b < b_end;
-      int z[2 * MT];
+      Acts16<NP> a[2][NT];
+      unsigned z[2 * MT];
       float sc[2 * MT];
-      Raw16<NP> raw[2][NT];
       if (mine) {
-        const long long gi = sz0 + b / per_group;
-#pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-          const long long e = gi + (long long)(8 * min(i, eights)) * p.w.n_g;
-          z[i] = p.w.zeros[e], sc[i] = p.w.scales[e];
-        }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) raw[h][n].load(x[n] + 128 * b + 32 * q + 16 * h);
+          for (int n = 0; n < NT; ++n) pieces16<BITS>(next.x[h][n], a[h][n]);
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) z[i] = zero_word(next.z[i], BITS), sc[i] = next.s[i];
+        if (b + 8 < b_end) fetch(b + 8);
       }
-      const bool landed = __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * s, (st / p.stages) & 1u, &gave_up, &g_few_error));
+      const bool landed = __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * s, phase, &gave_up, &g_few_error));
       if (mine && landed) {  // (a wait that gave up leaves its share out; nobody skips a barrier)
-        Acts16<NP> a[2][NT];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) pieces16<BITS>(raw[h][n], a[h][n]);
-        const unsigned char* at = ring + s * STAGE + g * PITCH + (4 * warp + q) * 4 * BITS;
+        const unsigned char* stage = ring + s * STAGE;
+        const int at = (4 * warp + q) * 4 * BITS;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           unsigned w0[BITS], w1[BITS];
-          load_words<BITS>(at + 16 * m * PITCH, w0);
-          load_words<BITS>(at + (16 * m + 8) * PITCH, w1);
-          const unsigned z0 = zero_word(z[2 * m], BITS), z1 = zero_word(z[2 * m + 1], BITS);
+          load_words<BITS, RC>(stage, 16 * m + g, at, w0);
+          load_words<BITS, RC>(stage, 16 * m + 8 + g, at, w1);
           float acc[NT][4] = {};
-          few_step16<BITS, 0, NT, NP>(w0, w1, z0, z1, a[0], acc);
-          few_step16<BITS, 1, NT, NP>(w0, w1, z0, z1, a[1], acc);
+          few_step16<BITS, 0, NT, NP>(w0, w1, z[2 * m], z[2 * m + 1], a[0], acc);
+          few_step16<BITS, 1, NT, NP>(w0, w1, z[2 * m], z[2 * m + 1], a[1], acc);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -283,8 +294,9 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
       }
       if (st + p.stages < n_st) {
         __syncthreads();
-        fill(st + p.stages);
+        if (threadIdx.x == 0) fill(st + p.stages);
       }
+      if (++s == p.stages) s = 0, phase ^= 1u;
     }
     __syncthreads();  // the ring becomes the sums'
   } else {
@@ -366,17 +378,17 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
   if (cs > 1) cluster_barrier();  // nobody leaves while its sums are read
 }
 
-template <int BITS, int NT, int NP, bool NARROW, typename T>
-tb_status launch_few(PackedFew p, cudaStream_t st) {
-  constexpr int MT = BITS <= 4 && NP * NT <= 3 ? 4 : 2, RC = 16 * MT;  // what 128 registers hold
-  constexpr int sums = 8 * RC * 8 * NT * 4, stage = NARROW ? 1 : RC * 9 * 16 * BITS, room = NT * NP == 1 ? 110 * 1024 : 220 * 1024;
+template <int BITS, int MT, int NT, int NP, bool NARROW, typename T>
+tb_status launch_few_rows(PackedFew p, cudaStream_t st) {
+  constexpr int RC = 16 * MT;
+  constexpr int sums = 8 * RC * 8 * NT * 4, stage = NARROW ? 1 : RC * 128 * BITS, room = (NT * NP == 1 ? 108 : 216) * 1024;
   auto kern = k_packed_few<BITS, MT, NT, NP, NARROW, T>;
   static bool configured[64] = {false};
   int dev = 0;
   TB_CUDA_CHECK(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return TB_ERR_CUDA;
   if (!configured[dev]) {
-    TB_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, room));
+    TB_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, room + 1024));
     configured[dev] = true;
   }
   const int tiles = (p.w.d_out + RC - 1) / RC, blocks = (p.n_tok + 8 * NT - 1) / (8 * NT);
@@ -387,24 +399,42 @@ tb_status launch_few(PackedFew p, cudaStream_t st) {
   const int n_st = ((units + cs - 1) / cs + 7) / 8, fit = room / stage;
   p.stages = NARROW ? 1 : n_st < fit ? n_st : fit;
   if (p.stages > FEW_STAGES_MAX) p.stages = FEW_STAGES_MAX;
-  const int smem = NARROW || p.stages * stage < sums ? sums : p.stages * stage;
+  const int smem = NARROW ? sums : (p.stages * stage < sums ? sums : p.stages * stage) + 1024;
+  CUtensorMap map = {};
+  if (!NARROW)
+    TB_TRY(make_map_2d(&map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, p.w.packed, (unsigned long long)p.w.words, (unsigned long long)p.w.d_out, 32, RC,
+                       CU_TENSOR_MAP_SWIZZLE_128B));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * cs), (unsigned)blocks);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)cs;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  int n = 0;
+  if (cs > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)cs;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  if (p.ad.n) {  // beside the kernel that makes x A^T, which started when all before it had ended
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = p.ad.n ? 2 : 1;  // beside the kernel that makes x A^T, which started when all before it had ended
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, p));
+  cfg.numAttrs = n;
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, p, map));
   TB_LAUNCH_CHECK();
   return TB_OK;
+}
+
+template <int BITS, int NT, int NP, bool NARROW, typename T>
+tb_status launch_few(const PackedFew& p, cudaStream_t st) {
+  constexpr int TOP = BITS <= 4 && NP * NT <= 3 ? 4 : 2;  // what the registers hold
+  const long long wanted = 3ll * (sm_count() > 0 ? sm_count() : 148) / 2, blocks = (p.n_tok + 8 * NT - 1) / (8 * NT);
+  if (TOP == 4 && (p.w.d_out + 63) / 64 * blocks >= wanted) return launch_few_rows<BITS, TOP, NT, NP, NARROW, T>(p, st);
+  if ((p.w.d_out + 31) / 32 * blocks >= wanted) return launch_few_rows<BITS, 2, NT, NP, NARROW, T>(p, st);
+  return launch_few_rows<BITS, 1, NT, NP, NARROW, T>(p, st);
 }
 
 template <int NT, int NP, typename T>
