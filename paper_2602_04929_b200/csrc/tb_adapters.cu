@@ -1,7 +1,6 @@
 // Low-rank adapters of many requests, bf16 activations: the narrow products x A_i^T (k_adapter_low) and the gradients of the
-// adapters' matrices (k_adapter_grad), both on mma.sync: a narrow product has a few dozen products for every value it reads, far
-// below what the tensor cores need to be kept busy, so both are bound by reading the activations (or, with a token or two for an
-// adapter, the adapters) once.
+// adapters' matrices (k_adapter_grad).  A narrow product has a few dozen products for every value it reads, far below what keeps
+// the tensor cores busy, so both are bound by reading the activations (or, with a token or two for an adapter, the adapters) once.
 #include "tb_packed.cuh"
 #include "tb_pair.cuh"
 
@@ -164,144 +163,212 @@ tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_
 
 // ------------------------------------------------------------------------------------------ gradients
 //
-// G_i [rank][width] = scale_i sum over i's tokens of low_t^T in_t.  A CTA has 128 columns of one adapter and, as one of a cluster,
-// every cs-th piece of 64 tokens; rows are the rank (M), columns N, tokens the contraction.  The input's tile goes to shared
-// memory by cp.async (8-bit codes through registers, as bf16 integers) and is read with transposing loads; low is split into three
-// bf16 pieces, all 24 bits of it, times the codes' scale of its token and these 128 columns.  The CTAs' sums are added in a fixed
-// order through distributed shared memory.
+// G_i [rank][width] = scale_i sum over i's tokens of low_t^T in_t, on tcgen05: 128 columns of the input are the rows M of the tile,
+// the rank its columns N, tokens the contraction, 64 of them a stage.  Both operands are written to shared memory by the producer
+// warps, as they are stored (M- and N-major, 128-byte swizzle): the input as it is, or its 8-bit codes as bf16 integers; low as
+// three bf16 pieces side by side (N = 3 RP), all 24 bits of it, times the codes' scale of its token and these 128 columns.  Tokens
+// behind the end of a request are zeros in both, so nothing of another request gets in.  The kernel is bound by reading the input
+// and, at high ranks, by making the pieces.  A CTA has one adapter's columns and, as one of a cluster, every cs-th piece of 64
+// tokens; accumulations end after 2048 tokens; the CTAs' sums are added in a fixed order through distributed shared memory.
 
-enum { AG_TOK = 64, AG_COLS = 128, AG_PIECES = 3 };
+enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 32, AG_THREADS = 288 };  // AG_PART: stages of an accumulation
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
-  const int n = in ? 16 : 0;  // the rest is filled with zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+static __device__ int g_grad_error = 0;
+
+// RP: the rank, rounded up to 16, 32, 64 or 128.
+template <int RP>
+struct GradShape {
+  enum {
+    N = 3 * RP,
+    BOXES = (N + 63) / 64,  // of 64 columns
+    A_BYTES = AG_TOK * AG_COLS * 2,
+    STAGE = A_BYTES + BOXES * AG_TOK * 128,
+    STAGES = RP == 16 ? 4 : RP == 64 ? 2 : 3,
+    TMEM = RP == 16 ? 64 : RP == 32 ? 128 : RP == 64 ? 256 : 512,
+    SUMS = RP * AG_COLS * 4,
+    SMEM = (STAGES * STAGE > SUMS ? STAGES * STAGE : SUMS) + 1024
+  };
+};
+
+__device__ __forceinline__ void sts8(uint32_t addr, unsigned a, unsigned b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
-__device__ __forceinline__ void ldsm4(uint32_t addr, unsigned (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+__device__ __forceinline__ void sts16(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, unsigned (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+__device__ __forceinline__ unsigned pair_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned*>(&v);
+}
+__device__ __forceinline__ float rest_of(float v, unsigned bits) {  // of v without its bf16 piece; nothing of what is not finite
+  const float f = __uint_as_float(bits);
+  return fabsf(f) <= 3.3895e38f ? v - f : 0.0f;
 }
 
-// RT: rows of the rank in sixteens.  Shared memory: two input tiles [64 tokens][128 columns] of bf16, the pieces of low
-// [piece][16 RT][64 tokens], both in 16-byte units swizzled by their row.
-template <int RT, bool EIGHT>
-__global__ void __launch_bounds__(256) k_adapter_grad(Adapt ad, const void* __restrict__ in, const float* __restrict__ in_scales,
-                                                      const float* __restrict__ low, int n_tok, int width, float* __restrict__ G) {
-  constexpr int ROWS = 16 * RT;
-  extern __shared__ __align__(128) unsigned char ag_smem[];
+template <int RP, bool EIGHT>
+__global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
+    k_adapter_grad(Adapt ad, const void* __restrict__ in, const float* __restrict__ in_scales, const float* __restrict__ low, int n_tok,
+                   int width, float* __restrict__ G) {
+  using S = GradShape<RP>;
+  extern __shared__ unsigned char ag_raw[];
+  __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int gave_up;
   __shared__ int2 piece[256];
   __shared__ int n_piece, wsum[8];
-  const uint32_t xs = smem_u32(ag_smem), ls = xs + 2 * AG_TOK * AG_COLS * 2;
-  float* sum = reinterpret_cast<float*>(ag_smem);  // after the last tile: [ROWS][128]
+  const uint32_t base = (smem_u32(ag_raw) + 1023u) & ~1023u;
+  float* sums = reinterpret_cast<float*>(ag_raw + (base - smem_u32(ag_raw)));  // after the last stage: [RP][128]
+  const uint32_t bar0 = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (S::STAGES + s); };
+  const uint32_t done_bar = bar0 + 16u * S::STAGES;
   uint32_t rank, cs;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
   const int c0 = (blockIdx.x / cs) * AG_COLS, id = blockIdx.y;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < S::STAGES; ++s) {
+      mbar_init(full_bar(s), 8);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(done_bar, 1);
+    gave_up = 0;
+    mbar_fence_init();
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((uint32_t)S::TMEM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
   const int n_run = (width + CKPT_RUN - 1) / CKPT_RUN;
-  float acc[RT][2][4] = {};
 
-  auto load_x = [&](int buf, int t, int n) {  // 64 tokens from t on, n of them inside
-    const uint32_t dst = xs + buf * (AG_TOK * AG_COLS * 2);
-    if constexpr (!EIGHT) {
+  // producers: a thread has 64 bytes of the input's tile (16-byte units e = tid + 256 i), and fours of low, neighbours side by side
+  uint4 xv[EIGHT ? 2 : 4];
+  float lv[RP / 4], fv[RP / 16];
+  auto fetch = [&](int t, int n) {  // 64 tokens from t on, n of them inside
+    if constexpr (EIGHT) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int e = tid + 256 * i, row = e >> 3, u = e & 7;
+        const signed char* src = static_cast<const signed char*>(in) + (long long)(t + row) * width + c0 + 16 * u;
+        xv[i] = row < n && c0 + 16 * u < width ? __ldcs(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+      }
+    } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = tid + 256 * i, row = e >> 4, u = e & 15;
-        const bool ok = row < n && c0 + 8 * u < width;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(in) + (ok ? (long long)(t + row) * width + c0 + 8 * u : 0);
-        cp_async16(dst + row * 256 + ((u ^ (row & 7)) << 4), src, ok);
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(in) + (long long)(t + row) * width + c0 + 8 * u;
+        xv[i] = row < n && c0 + 8 * u < width ? __ldcs(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < RP / 16; ++k) {
+      const int e = tid + 256 * k, lt = e / (RP / 4), r = 4 * (e % (RP / 4));
+      const bool in4 = lt < n && r < ad.rank;
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (in4) v = __ldg(reinterpret_cast<const float4*>(low + (long long)(t + lt) * ad.rank + r));
+      if (EIGHT) fv[k] = in4 ? __ldg(in_scales + (long long)(t + lt) * n_run + c0 / CKPT_RUN) : 0.0f;
+      lv[4 * k] = v.x, lv[4 * k + 1] = v.y, lv[4 * k + 2] = v.z, lv[4 * k + 3] = v.w;
+    }
   };
-  uint4 codes[2];
-  auto fetch_codes = [&](int t, int n) {
+  auto store = [&](uint32_t stage) {
     if constexpr (EIGHT) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int e = tid + 256 * i, row = e >> 3, u = e & 7;
-        const bool ok = row < n && c0 + 16 * u < width;
-        codes[i] = ok ? __ldcs(reinterpret_cast<const uint4*>(static_cast<const signed char*>(in) + (long long)(t + row) * width + c0 + 16 * u))
-                      : make_uint4(0, 0, 0, 0);
-      }
-    }
-  };
-  auto store_codes = [&](int buf) {
-    if constexpr (EIGHT) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int e = tid + 256 * i, row = e >> 3, u = e & 7;
-        const unsigned w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+        const unsigned w[4] = {xv[i].x, xv[i].y, xv[i].z, xv[i].w};
         unsigned o[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const unsigned v = w[k >> 1] >> (16 * (k & 1));
-          const __nv_bfloat162 b = __floats2bfloat162_rn((float)(signed char)(v & 0xffu), (float)(signed char)((v >> 8) & 0xffu));
-          o[k] = *reinterpret_cast<const unsigned*>(&b);
+          // codes as floats: the byte, its sign flipped, in the low mantissa bits of 2^23, less 2^23 + 128
+          const unsigned v = (w[k >> 1] ^ 0x80808080u) >> (16 * (k & 1));
+          const float a = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7540)) - 8388736.0f;
+          const float b = __uint_as_float(__byte_perm(v, 0x4B000000u, 0x7541)) - 8388736.0f;
+          o[k] = pair_bf16(a, b);
         }
+        const uint32_t at = stage + (u >> 2) * 8192 + row * 128;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<uint4*>(ag_smem + buf * (AG_TOK * AG_COLS * 2) + row * 256 + (((2 * u + h) ^ (row & 7)) << 4)) =
-              make_uint4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
+          sts16(at + ((((u & 3) * 2 + h) ^ (row & 7)) << 4), make_uint4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]));
       }
-    }
-  };
-  // a thread has a token and every fourth group of 4 of the rank
-  const int lt = tid & 63, lq = tid >> 6;
-  float4 lv[RT];
-  auto fetch_low = [&](int t, int n) {
-    const bool ok = lt < n;
-    float f = 1.0f;
-    if (EIGHT && ok) f = __ldg(in_scales + (long long)(t + lt) * n_run + c0 / CKPT_RUN);
-#pragma unroll
-    for (int k = 0; k < RT; ++k) {
-      const int r = 16 * k + 4 * lq;
-      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (ok && r < ad.rank) {
-        v = *reinterpret_cast<const float4*>(low + (long long)(t + lt) * ad.rank + r);
-        if (EIGHT) v.x *= f, v.y *= f, v.z *= f, v.w *= f;
-      }
-      lv[k] = v;
-    }
-  };
-  auto store_low = [&]() {
-#pragma unroll
-    for (int k = 0; k < RT; ++k) {
-      const float v[4] = {lv[k].x, lv[k].y, lv[k].z, lv[k].w};
+    } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = 16 * k + 4 * lq + i;
-        float left = v[i];
+        const int e = tid + 256 * i, row = e >> 4, u = e & 15;
+        sts16(stage + (u >> 3) * 8192 + row * 128 + (((u & 7) ^ (row & 7)) << 4), xv[i]);
+      }
+    }
 #pragma unroll
-        for (int p = 0; p < AG_PIECES; ++p) {
-          const __nv_bfloat16 b = __float2bfloat16(left);
-          const float f = __bfloat162float(b);
-          left = fabsf(f) <= 3.3895e38f ? left - f : 0.0f;  // nothing is left of what is not finite
-          *reinterpret_cast<__nv_bfloat16*>(ag_smem + 2 * AG_TOK * AG_COLS * 2 + ((p * ROWS + r) << 7) + (((lt >> 3) ^ (r & 7)) << 4) + 2 * (lt & 7)) = b;
+    for (int k = 0; k < RP / 16; ++k) {
+      const int e = tid + 256 * k, lt = e / (RP / 4), r = 4 * (e % (RP / 4));
+      float v[4] = {lv[4 * k], lv[4 * k + 1], lv[4 * k + 2], lv[4 * k + 3]};
+      if (EIGHT) v[0] *= fv[k], v[1] *= fv[k], v[2] *= fv[k], v[3] *= fv[k];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        const unsigned a = pair_bf16(v[0], v[1]), b = pair_bf16(v[2], v[3]);
+        const int n = p * RP + r;
+        sts8(stage + S::A_BYTES + (n >> 6) * 8192 + lt * 128 + ((((n & 63) >> 3) ^ (lt & 7)) << 4) + (n & 7) * 2, a, b);
+        if (p < 2) {
+          v[0] = rest_of(v[0], a << 16), v[1] = rest_of(v[1], a & 0xffff0000u);
+          v[2] = rest_of(v[2], b << 16), v[3] = rest_of(v[3], b & 0xffff0000u);
         }
       }
     }
+  };
+
+  // the MMAs of a stage, and after the last of an accumulation its end: by warp 8
+  const uint32_t idesc = idesc_bf16_mn(128, RP == 128 ? 192 : S::N);
+  float acc[RP / 2];  // producers: lane's column of the input, half of the rank
+#pragma unroll
+  for (int i = 0; i < RP / 2; ++i) acc[i] = 0.0f;
+  uint32_t it = 0, parts = 0;
+  bool ok = true;
+  auto drain = [&]() {  // the finished accumulation into the registers (warps 0-7)
+    ok = __all_sync(0xffffffffu, mbar_wait(done_bar, parts & 1u, &gave_up, &g_grad_error));
+    ++parts;
+    if (!ok) return;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+    for (int p = 2; p >= 0; --p)
+#pragma unroll
+      for (int c = 0; c < RP / 2; c += 8) {
+        uint32_t r[8];
+        tmem_ld_32x8(tmem + ((uint32_t)((warp & 3) * 32) << 16) + p * RP + (warp >> 2) * (RP / 2) + c, r);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[c + i] += __uint_as_float(r[i]);
+      }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   };
 
   for (int j0 = 0; j0 < ad.n_req; j0 += 256) {
     // the adapter's requests among these 256, in their order
     int b = 0, e = 0;
-    if (j0 + tid < ad.n_req && ad.ids[j0 + tid] == id) {
-      b = max(0, ad.starts[j0 + tid]);
-      e = min(n_tok, ad.starts[j0 + tid + 1]);
+    if (warp < 8) {
+      if (j0 + tid < ad.n_req && ad.ids[j0 + tid] == id) {
+        b = max(0, ad.starts[j0 + tid]);
+        e = min(n_tok, ad.starts[j0 + tid + 1]);
+      }
+      const unsigned m = __ballot_sync(0xffffffffu, e > b);
+      if (lane == 0) wsum[warp] = __popc(m);
+      __syncwarp();
     }
-    const unsigned m = __ballot_sync(0xffffffffu, e > b);
-    if (lane == 0) wsum[warp] = __popc(m);
     __syncthreads();
-    int at = __popc(m & ((1u << lane) - 1u)), all = 0;
+    if (warp < 8) {
+      const unsigned m = __ballot_sync(0xffffffffu, e > b);
+      int at = __popc(m & ((1u << lane) - 1u)), all = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (k < warp) at += wsum[k];
-      all += wsum[k];
+      for (int k = 0; k < 8; ++k) {
+        if (k < warp) at += wsum[k];
+        all += wsum[k];
+      }
+      if (e > b) piece[at] = make_int2(b, e);
+      if (tid == 0) n_piece = all;
     }
-    if (e > b) piece[at] = make_int2(b, e);
-    if (tid == 0) n_piece = all;
     __syncthreads();
     // this CTA's pieces of 64 tokens: every cs-th, counted through these requests
     int rq = 0, t = 0;
@@ -318,68 +385,64 @@ __global__ void __launch_bounds__(256) k_adapter_grad(Adapt ad, const void* __re
     };
     if (n_piece > 0) t = piece[0].x;
     advance((int)rank);
-    int buf = 0;
-    if (rq < n_piece) {
-      const int n = min(AG_TOK, piece[rq].y - t);
-      load_x(0, t, n);
-      fetch_codes(t, n);
-      fetch_low(t, n);
-    }
-    while (rq < n_piece) {
-      store_low();
-      store_codes(buf);
+    if (warp < 8 && rq < n_piece) fetch(t, min(AG_TOK, piece[rq].y - t));
+    uint32_t in_part = 0;
+    while (rq < n_piece && ok) {
+      const uint32_t s = it % S::STAGES, ph = (it / S::STAGES) & 1u;
+      const uint32_t stage = base + s * S::STAGE;
       advance((int)cs);
-      const bool more = rq < n_piece;
-      const int n = more ? min(AG_TOK, piece[rq].y - t) : 0;
-      if (more) {
-        load_x(buf ^ 1, t, n);
-        fetch_codes(t, n);
-        fetch_low(t, n);
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-      } else {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-      }
-      __syncthreads();
-      const uint32_t xb = xs + buf * (AG_TOK * AG_COLS * 2);
-#pragma unroll
-      for (int kk = 0; kk < AG_TOK / 16; ++kk) {
-        unsigned x[4];  // b0, b1 of the warp's two column tiles
-        {
-          const int row = 16 * kk + (lane & 15), u = 2 * warp + (lane >> 4);
-          ldsm4_t(xb + row * 256 + ((u ^ (row & 7)) << 4), x);
+      const bool more = rq < n_piece, last = !more || in_part == AG_PART - 1;
+      if (warp < 8) {
+        ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(s), ph ^ 1u, &gave_up, &g_grad_error));
+        if (ok) {
+          store(stage);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(full_bar(s));
+          // (loads after the fence: it waits for all that its thread has in flight)
+          if (more) fetch(t, min(AG_TOK, piece[rq].y - t));
+          if (last) drain();
         }
+      } else {
+        ok = __all_sync(0xffffffffu, mbar_wait(full_bar(s), ph, &gave_up, &g_grad_error));
+        if (ok && elect_one()) {
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-        for (int p = 0; p < AG_PIECES; ++p)
-#pragma unroll
-          for (int k = 0; k < RT; ++k) {
-            unsigned a[4];
-            const int r = 16 * k + (lane & 7) + 8 * ((lane >> 3) & 1), u = 2 * kk + (lane >> 4);
-            ldsm4(ls + ((p * ROWS + r) << 7) + ((u ^ (r & 7)) << 4), a);
-            mma_bf16(acc[k][0], a[0], a[1], a[2], a[3], x[0], x[1]);
-            mma_bf16(acc[k][1], a[0], a[1], a[2], a[3], x[2], x[3]);
+          for (int kk = 0; kk < AG_TOK / 16; ++kk) {
+            const uint64_t a = smem_desc_mn_sw128(stage + kk * 2048);
+            const uint32_t first = in_part > 0 || kk > 0 ? 1u : 0u;
+            umma_bf16(tmem, a, smem_desc_mn_sw128(stage + S::A_BYTES + kk * 2048), idesc, first);
+            if (RP == 128) umma_bf16(tmem + 192, a, smem_desc_mn_sw128(stage + S::A_BYTES + 3 * 8192 + kk * 2048), idesc, first);
           }
+          umma_commit(empty_bar(s));
+          if (last) umma_commit(done_bar);
+        }
+        __syncwarp();
       }
-      __syncthreads();
-      buf ^= 1;
+      in_part = last ? 0 : in_part + 1;
+      ++it;
+      // the next accumulation overwrites the drained one: its first stage is handed over by every producer after its drain
     }
+    __syncthreads();
   }
-  // (every thread is past its last tile: the sums may take its place)
-  const int g = lane >> 2, q = lane & 3;
+  // (every MMA has been drained: the sums may take the stages' place)
+  if (warp < 8) {
+    const int c = (warp & 3) * 32 + lane;
 #pragma unroll
-  for (int k = 0; k < RT; ++k)
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) sum[(16 * k + g + 8 * (c >> 1)) * AG_COLS + 16 * warp + 8 * n + 2 * q + (c & 1)] = acc[k][n][c];
+    for (int i = 0; i < RP / 2; ++i) sums[((warp >> 2) * (RP / 2) + i) * AG_COLS + c] = acc[i];
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::TMEM) : "memory");
   if (cs > 1) cluster_barrier();
   const float sc = ad.scale[id];
-  for (int e = tid + 256 * rank; e < ROWS * AG_COLS; e += 256 * cs) {
+  const uint32_t mine = smem_u32(sums);
+  for (int e = tid + AG_THREADS * (int)rank; e < RP * AG_COLS; e += AG_THREADS * (int)cs) {
     const int r = e / AG_COLS, c = e % AG_COLS;
     if (r >= ad.rank || c0 + c >= width) continue;
     float v = 0.0f;
     for (uint32_t k = 0; k < cs; ++k) {
-      const float p = cs > 1 ? ld_cluster(map_to_rank(xs + 4u * e, k)) : sum[e];
+      const float p = cs > 1 ? ld_cluster(map_to_rank(mine + 4u * e, k)) : sums[e];
       v = k ? v + p : p;
     }
     G[((long long)id * ad.rank + r) * width + c0 + c] = sc * v;
@@ -387,25 +450,35 @@ __global__ void __launch_bounds__(256) k_adapter_grad(Adapt ad, const void* __re
   if (cs > 1) cluster_barrier();
 }
 
-template <int RT, bool EIGHT>
+int adapter_grad_error_read_clear() {
+  int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_grad_error, sizeof(int)) != cudaSuccess) return -1;
+  if (v) {
+    int z = 0;
+    cudaMemcpyToSymbol(g_grad_error, &z, sizeof(int));
+  }
+  return v;
+}
+
+template <int RP, bool EIGHT>
 static tb_status launch_grad(const Adapt& ad, const void* in, const float* in_scales, const float* low, int n_tok, int width, float* G,
                              cudaStream_t st) {
-  constexpr int tiles_bytes = 2 * AG_TOK * AG_COLS * 2 + AG_PIECES * 16 * RT * AG_TOK * 2, sum_bytes = 16 * RT * AG_COLS * 4;
-  constexpr int smem = tiles_bytes > sum_bytes ? tiles_bytes : sum_bytes;
+  constexpr int smem = GradShape<RP>::SMEM;
   static bool configured[64] = {false};
   int dev = 0;
   TB_CUDA_CHECK(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return TB_ERR_CUDA;
   if (!configured[dev]) {
-    TB_CUDA_CHECK(cudaFuncSetAttribute(k_adapter_grad<RT, EIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    TB_CUDA_CHECK(cudaFuncSetAttribute(k_adapter_grad<RP, EIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     configured[dev] = true;
   }
   const int cols = (width + AG_COLS - 1) / AG_COLS, sms = sm_count() > 0 ? sm_count() : 148;
-  int cs = 1;  // CTAs along the tokens until about two an SM
-  while (cs < 8 && (long long)cols * ad.n * cs * 2 <= 2 * sms && n_tok / ad.n / (2 * cs) >= AG_TOK) cs *= 2;
+  // CTAs along the tokens until an adapter that had nearly all of them would fill the GPU, while an even share is a stage at least
+  int cs = 1;
+  while (cs < 8 && cols * cs * 2 <= 2 * sms && n_tok / ad.n / (2 * cs) >= AG_TOK) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(cols * cs), (unsigned)ad.n);
-  cfg.blockDim = dim3(256);
+  cfg.blockDim = dim3(AG_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -415,7 +488,7 @@ static tb_status launch_grad(const Adapt& ad, const void* in, const float* in_sc
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_grad<RT, EIGHT>, ad, in, in_scales, low, n_tok, width, G));
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_grad<RP, EIGHT>, ad, in, in_scales, low, n_tok, width, G));
   TB_LAUNCH_CHECK();
   return TB_OK;
 }
@@ -423,10 +496,10 @@ static tb_status launch_grad(const Adapt& ad, const void* in, const float* in_sc
 template <bool EIGHT>
 static tb_status grad_of_rank(const Adapt& ad, const void* in, const float* in_scales, const float* low, int n_tok, int width, float* G,
                               cudaStream_t st) {
-  if (ad.rank <= 16) return launch_grad<1, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
-  if (ad.rank <= 32) return launch_grad<2, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
-  if (ad.rank <= 64) return launch_grad<4, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
-  return launch_grad<8, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
+  if (ad.rank <= 16) return launch_grad<16, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
+  if (ad.rank <= 32) return launch_grad<32, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
+  if (ad.rank <= 64) return launch_grad<64, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
+  return launch_grad<128, EIGHT>(ad, in, in_scales, low, n_tok, width, G, st);
 }
 
 // `in` bf16, or 8-bit codes where in_scales is given.

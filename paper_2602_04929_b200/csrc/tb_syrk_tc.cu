@@ -258,6 +258,7 @@ int packed_fwd_error_read_clear();  // the products with bit-packed weights (tb_
 int packed_bwd_error_read_clear();  // tb_packed_tc_bwd.cu,
 int packed_few_bf16_1_error_read_clear();  // tb_packed_few_*.cu)
 int packed_few_bf16_2_error_read_clear();
+int adapter_grad_error_read_clear();  // the adapters' gradients (tb_adapters.cu)
 int packed_few_f32_1_error_read_clear();
 int packed_few_f32_2_error_read_clear();
 int pair_error_read_clear();   // and of the CTA-pair form of the Hessian kernel (tb_syrk_tc2.cu)
@@ -305,9 +306,9 @@ extern "C" int tb_device_error_flag(void) {
   const int q = tb::pair_error_read_clear();
   const int pf = tb::packed_fwd_error_read_clear();
   const int pb = tb::packed_bwd_error_read_clear();
-  const int few[4] = {tb::packed_few_bf16_1_error_read_clear(), tb::packed_few_bf16_2_error_read_clear(),
+  const int few[5] = {tb::adapter_grad_error_read_clear(), tb::packed_few_bf16_1_error_read_clear(), tb::packed_few_bf16_2_error_read_clear(),
                       tb::packed_few_f32_1_error_read_clear(), tb::packed_few_f32_2_error_read_clear()};
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 5; ++i) {
     if (few[i] < 0) return -1;
     v |= few[i];
   }
