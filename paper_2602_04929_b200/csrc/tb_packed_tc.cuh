@@ -64,11 +64,11 @@ struct Parts {
   }
 };
 
-// c - z, exact, times s, rounded to bf16 once
-__device__ __forceinline__ void scale8(unsigned (&o)[4], float s) {
+// c - z, exact, times s, rounded to bf16: s as two bf16 pieces, the smaller product rounded first, 2^-8 of the last place of the
+// result; the fused multiply-add rounds the sum
+__device__ __forceinline__ void scale8(unsigned (&o)[4], unsigned hi, unsigned lo) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    o[i] = bf2(__floats2bfloat162_rn(__uint_as_float(o[i] << 16) * s, __uint_as_float(o[i] & 0xffff0000u) * s));
+  for (int i = 0; i < 4; ++i) o[i] = bf2(__hfma2(bf2(o[i]), bf2(hi), __hmul2(bf2(o[i]), bf2(lo))));
 }
 
 __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
@@ -108,12 +108,12 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 template <int BITS, int C, bool BACK>
-__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const float (&s)[2], uint32_t row_addr,
+__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const unsigned (&s)[2][2], uint32_t row_addr,
                                            uint32_t sw) {
   if constexpr (C < 8) {
     unsigned o[4];
     decode8<BITS, 8 * C>(w, z[C / 4], o);
-    if constexpr (BACK) scale8(o, s[C / 4]);
+    if constexpr (BACK) scale8(o, s[C / 4][0], s[C / 4][1]);
     sts16(row_addr + ((C ^ sw) << 4), o);
     decode_row<BITS, C + 1, BACK>(w, z, s, row_addr, sw);
   }
@@ -250,7 +250,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
         const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
-        parts.start(c.k0);
+        // accumulations of one length: the same steps of 16 each, no column to keep
+        const int regular = parts.part % 64 == 0 && group % parts.part == 0 && c.k0 % parts.part == 0 && c.k1 % parts.part == 0 ? parts.part >> 4 : 0;
+        if (!regular) parts.start(c.k0);
         int k = c.k0, left = 0, todo = (c.k1 - c.k0 + 15) >> 4;  // column; steps of 16 of the accumulation under way, of the tile
         for (int st = 0; st < n_st + c.lora; ++st) {
           ok = mbar_wait_warp(full_bar(s), phase, abort_flag, &g_packed_error);
@@ -264,8 +266,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
             if (left == 0) {
               ok = acc_free();
               if (!ok) break;
-              left = (min(parts.end, c.k1) - k + 15) >> 4;
-              parts.next();
+              left = regular;
+              if (!regular) {
+                left = (min(parts.end, c.k1) - k + 15) >> 4;
+                parts.next();
+              }
               more = 0;
             }
             if (left >= 4 && todo >= 4) {  // the whole stage in one accumulation
@@ -384,7 +389,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           // outside the matrix the words are zeros and any zero-point gives finite values, which meet zeros or are not stored
           const int half = BACK ? tid >> 6 : i;  // of the unit's 128 columns
           unsigned w[2 * BITS], z[2];
-          float sc[2] = {0.0f, 0.0f};
+          unsigned sc[2][2] = {};
           if constexpr (BITS % 2 == 0) {
 #pragma unroll
             for (int e = 0; e < BITS / 2; ++e) {
@@ -402,7 +407,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           for (int h = 0; h < 2; ++h) {
             const int o = (one_sz ? 0 : 2 * half + h) * Ring::ROWS * 4 + my_row * 4;
             z[h] = *reinterpret_cast<const unsigned*>(q + Ring::Z + o);
-            if (BACK) sc[h] = *reinterpret_cast<const float*>(q + Ring::S + o);
+            if (BACK) {
+              const float v = *reinterpret_cast<const float*>(q + Ring::S + o);
+              sc[h][0] = bf2(__float2bfloat162_rn(v));
+              sc[h][1] = bf2(__float2bfloat162_rn(v - __uint_as_float(sc[h][0] << 16)));
+            }
           }
           if (i == here - 1) {
             __syncwarp();
