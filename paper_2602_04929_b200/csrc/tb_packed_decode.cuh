@@ -38,7 +38,8 @@ __device__ __forceinline__ unsigned zero_word(int z, int bits) {
 }
 // Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
 // is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)
-// is joined with itself 16 - b bits higher.  Eight bits go through float.
+// is joined with itself 16 - b bits higher (its top code masked off below, where it would meet the copy's first).  Eight bits go
+// through float.
 template <int BITS, int N>
 __device__ __forceinline__ unsigned apart(unsigned f) {  // f: N codes; a product where the two do not overlap, else an or
   if constexpr (N * BITS <= 16 - BITS)
@@ -55,7 +56,21 @@ __device__ __forceinline__ void decode8(const unsigned (&w)[N], unsigned z, unsi
       const float a = __uint_as_float(0x4B000000u | (v & 0xffu)) - __uint_as_float(z), b = __uint_as_float(0x4B000000u | ((v >> 8) & 0xffu)) - __uint_as_float(z);
       o[i] = bf2(__floats2bfloat162_rn(a, b));
     }
-  } else if constexpr (BITS <= 4) {
+  } else if constexpr (BITS == 2) {
+    // all eight codes at once; those 4 bits up are 8 + c with the exponent of 8
+    const unsigned v = C0 % 16 ? w[C0 >> 4] >> 16 : w[C0 >> 4], y = v * 16384u + (v & 0x3fffu);
+    const __nv_bfloat162 z4 = __hadd2(bf2(z), __float2bfloat162_rn(120.0f));
+    o[0] = bf2(__hadd2(bf2(masked(y, 0x00030003u, 0x43004300u)), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(masked(y, 0x00300030u, 0x41004100u)), z4));
+    o[2] = bf2(__hadd2(bf2(masked(y >> 8, 0x00030003u, 0x43004300u)), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(masked(y >> 8, 0x00300030u, 0x41004100u)), z4));
+  } else if constexpr (BITS == 4) {
+    const unsigned v = w[C0 >> 3], y0 = v * 4096u + (v & 0xfffu), y1 = (v >> 16) * 4096u + ((v >> 16) & 0xfffu);
+    o[0] = bf2(__hadd2(bf2(masked(y0, 0x000f000fu, 0x43004300u)), bf2(z)));
+    o[1] = bf2(__hadd2(bf2(masked(y0 >> 8, 0x000f000fu, 0x43004300u)), bf2(z)));
+    o[2] = bf2(__hadd2(bf2(masked(y1, 0x000f000fu, 0x43004300u)), bf2(z)));
+    o[3] = bf2(__hadd2(bf2(masked(y1 >> 8, 0x000f000fu, 0x43004300u)), bf2(z)));
+  } else if constexpr (BITS == 3) {
     constexpr unsigned m = ((1u << BITS) - 1u) * 0x10001u;
     const unsigned y0 = apart<BITS, 4>(field<C0 * BITS, 4 * BITS>(w)), y1 = apart<BITS, 4>(field<(C0 + 4) * BITS, 4 * BITS>(w));
     o[0] = bf2(__hadd2(bf2(masked(y0, m, 0x43004300u)), bf2(z)));

@@ -35,8 +35,14 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
     __syncthreads();
     for (int i = warp; i < 32; i += 8)
       if (g0 + i < p.w.n_g) {  // rows_pad is a multiple of 32
-        p.st[(long long)(g0 + i) * p.rows_pad + r0 + lane] = s[lane][i];
-        p.zt[(long long)(g0 + i) * p.rows_pad + r0 + lane] = z[lane][i];
+        const long long at = (long long)(g0 + i) * p.rows_pad + r0 + lane;
+        if (p.st) {
+          p.st[at] = s[lane][i];
+          p.zt[at] = z[lane][i];
+        } else {  // the scale's pieces: the first in the upper half
+          const float v = s[lane][i], hi = __bfloat162float(__float2bfloat16(v));
+          reinterpret_cast<uint2*>(p.zt)[at] = make_uint2(z[lane][i], bf2(__floats2bfloat162_rn(v - hi, hi)));
+        }
       }
     return;
   }
@@ -137,12 +143,12 @@ TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
   return best;
 }
 
-size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, char* ws, PackedTc* p) {
+size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, bool back, char* ws, PackedTc* p) {
   Bump b(ws);
   p->rows_pad = (w.d_out + 255) / 256 * 256;  // whole tiles of a CTA pair
   p->pitch = (w.words + 3) / 4 * 4;
-  p->st = b.take<float>((size_t)w.n_g * p->rows_pad);
-  p->zt = b.take<unsigned>((size_t)w.n_g * p->rows_pad);
+  p->st = back ? nullptr : b.take<float>((size_t)w.n_g * p->rows_pad);
+  p->zt = b.take<unsigned>((size_t)w.n_g * p->rows_pad * (back ? 2 : 1));
   p->words = p->pitch != w.words ? b.take<unsigned>((size_t)w.d_out * p->pitch) : w.packed;
   p->runs = ad.n && t.splits == 1 ? b.take<int4>(n_tok) : nullptr;
   p->n_runs = ad.n && t.splits == 1 ? b.take<int>(t.t_tiles) : nullptr;
@@ -172,7 +178,7 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   PackedTc p = {};
   p.n_cols = back ? w.d_in : w.d_out, p.n_sum = back ? w.d_out : w.d_in, p.n_tok = (int)n_tok;
   const TcPlan t = packed_tc_plan(p.n_tok, p.n_cols, p.n_sum);
-  packed_tc_carve(t, w, ad, p.n_tok, p.n_cols, static_cast<char*>(ws), &p);
+  packed_tc_carve(t, w, ad, p.n_tok, p.n_cols, back, static_cast<char*>(ws), &p);
   p.w = w, p.ad = ad, p.low = low, p.out = out;
   p.M = static_cast<const __nv_bfloat16*>(back ? ad.A : ad.B);
   p.n_tile = t.n_tile, p.m_tiles = t.m_tiles, p.t_tiles = t.t_tiles, p.splits = t.splits, p.split_len = t.split_len;

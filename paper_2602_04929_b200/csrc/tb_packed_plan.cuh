@@ -10,7 +10,6 @@ enum {
   PT_BK = 64,
   PT_A_BYTES = 128 * PT_BK * 2,
   PT_STAGE_BYTES = 2 * PT_A_BYTES,  // A, then B (at most 128 tokens)
-  PT_THREADS = 640,
   PT_PART = 2048,  // contraction columns of one accumulation at most
   PT_SMEM = 226 * 1024 + 512       // stages, ring, 1024 bytes to align them, 512 of barriers
 };
@@ -21,8 +20,8 @@ struct PackedTc {
   Adapt ad;
   const __nv_bfloat16* M;  // adapters' matrix of the result's columns, [adapter][rank][n_cols]
   const float* low;        // [n_tok][rank]
-  const float* st;         // scales [n_g][rows_pad], zeros behind d_out
-  const unsigned* zt;      // zero-points as the decoders take them, likewise
+  const float* st;         // forward: scales [n_g][rows_pad], zeros behind d_out
+  const unsigned* zt;      // zero-points as the decoders take them, likewise; backward each followed by its scale's two bf16 pieces
   const unsigned* words;   // the packed rows, `pitch` words apart (a multiple of 16 bytes)
   int rows_pad, pitch;
   const int4* runs;        // per token tile, from its first token's index on: first token, end, adapter
@@ -37,7 +36,7 @@ struct TcPlan {
 };
 TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum);
 // Scratch of a product from `ws` on (nullptr: only its size).
-size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, char* ws, PackedTc* p);
+size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, bool back, char* ws, PackedTc* p);
 tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat16* in, long long n_tok, __nv_bfloat16* out,
                             const float* low, bool back, void* ws, cudaStream_t st);
 tb_status packed_tc_forward(const PackedTc& p, const CUtensorMap& xmap, const CUtensorMap& wmap, int pairs, cudaStream_t st);

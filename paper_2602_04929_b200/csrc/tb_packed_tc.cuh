@@ -11,17 +11,19 @@
 // holds c - z, which bf16 has exactly, and the accumulator of a group (at most 2048 columns of it) is taken from one of two TMEM
 // buffers, scaled and added to float registers by the epilogue warps while the other buffer fills.  The product so has no rounding
 // but that of float sums.  Backward, a scale belongs to the contraction row: the weight s (c - z) is rounded to bf16 when it is
-// decoded, and accumulators are added to the registers every 2048 rows.
+// decoded, which costs more instructions, and the sum stays in tensor memory to its end, one buffer a tile.
 //
 // Adapters.  scale v M, v [tokens][rank] float, joins the sum as further contraction steps: slots of 16 for a run of tokens with one
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
 // into the tile as zero and is added by the epilogue to the run's own tokens, so that it reaches no other token.
 //
-// Roles (640 threads): warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and scales, warps 4-11 decode, two warpgroups in turn, warps 12-19
-// epilogue.  The decode warps have no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor
-// cores, waits for all that its thread has in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are
-// split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).  Every wait is
-// bounded as in the Hessian kernels.
+// Roles: warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and
+// scales, then the decode warps (forward two warpgroups, backward four, in turn), then the epilogue (forward eight warps, backward
+// four).  The decode warps have no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor cores,
+// waits for all that its thread has in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Forward,
+// registers are split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).
+// Every wait is bounded as in the Hessian kernels.  The MMA warp goes through two stages at a time where it can: its instructions
+// between the MMAs, on a scheduler shared with busy warps, are what limits it.
 #pragma once
 
 #include "tb_packed.cuh"
@@ -76,8 +78,8 @@ __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
 }
 
 // The packed words on their way to the decode warps: 128 columns of the CTA's 128 weight rows (forward, two stages) or of 64 weight
-// rows (backward, one stage), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points, and
-// backward scales.  A ring of STAGES such units.  Rows of 32, 64 and 128 bytes are swizzled, so that neighbouring threads' rows lie
+// rows (backward, one stage), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points,
+// backward each beside its scale.  A ring of STAGES such units.  Rows of 32, 64 and 128 bytes are swizzled, so that neighbouring threads' rows lie
 // in different banks.
 template <int BITS, bool BACK>
 struct Raw {
@@ -85,10 +87,9 @@ struct Raw {
     ROWS = BACK ? 64 : 128,
     ROW = 16 * BITS,
     Z = ROWS * ROW,
-    S = Z + 4 * ROWS * 4,
-    BYTES = (BACK ? S + 4 * ROWS * 4 : S),
+    BYTES = Z + 4 * ROWS * (BACK ? 8 : 4),
     PAD = (BYTES + 1023) & ~1023,  // swizzled rows start on a multiple of their pattern
-    MMA_STAGES = BITS <= 4 ? 6 : 5,
+    MMA_STAGES = BITS <= 4 ? 6 : 4,  // even: the MMA warp takes two at a time
     ROOM = PT_SMEM - 1024 - 512 - MMA_STAGES * PT_STAGE_BYTES,
     STAGES = ROOM / PAD < 8 ? ROOM / PAD : 8
   };
@@ -132,9 +133,25 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
   return *reinterpret_cast<const unsigned short*>(&lo);
 }
 
+// both halves of c += a pair times s
+__device__ __forceinline__ void fma_two(uint64_t& c, uint32_t a0, uint32_t a1, float s) {
+  asm("{\n\t.reg .b64 a, b;\n\t"
+      "mov.b64 a, {%1, %2};\n\t"
+      "mov.b64 b, {%3, %3};\n\t"
+      "fma.rn.f32x2 %0, a, b, %0;\n\t}"
+      : "+l"(c)
+      : "r"(a0), "r"(a1), "f"(s));
+}
+
+template <bool BACK>
+struct Roles {
+  enum { DECODE = BACK ? 4 : 2, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
+};
+
 template <int BITS, bool BACK>
-__global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+__global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
   using Ring = Raw<BITS, BACK>;
+  using R = Roles<BACK>;
   constexpr int STAGES = Ring::MMA_STAGES;
   extern __shared__ unsigned char pt_smem_raw[];
   const uint32_t raw = smem_u32(pt_smem_raw);
@@ -170,7 +187,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf_bar(b), 1);
-      mbar_init(acce_bar(b), 16);
+      mbar_init(acce_bar(b), 2 * R::EPILOGUE);
     }
     *abort_flag = 0;
     *odd_flag = 0;
@@ -202,12 +219,12 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
     r.k0 = r.split * p.split_len;
     r.k1 = min(p.n_sum, r.k0 + p.split_len);
     r.n_runs = p.n_runs ? p.n_runs[ti] : 0;
-    r.lora = (r.n_runs * nb * 2 + 3) >> 2;  // stages of four slots
+    r.lora = ((r.n_runs * nb * 2 + 7) >> 3) * 2;  // stages of four slots, an even number of them
     return r;
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (!BACK) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer: this CTA's half of the tokens ----------------
       uint32_t it = 0;
@@ -242,78 +259,90 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       const uint64_t b_main = smem_desc_k_sw128(base + PT_A_BYTES);
       constexpr uint32_t a_step = (BACK ? 2048 : 32) >> 4, l_step = 2048 >> 4, b_step = 32 >> 4;
       Parts parts(group);
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, &g_packed_error); };
       auto acc_free = [&]() {
-        const bool got = mbar_wait_warp(acce_bar(acc_it & 1u), ((acc_it >> 1) & 1u) ^ 1u, abort_flag, &g_packed_error);
+        const bool got = wait(acce_bar(acc_it & 1u), ((acc_it >> 1) & 1u) ^ 1u);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         return got;
+      };
+      auto four = [&](uint32_t d, uint64_t ad, uint64_t bd, uint32_t more) {
+        umma_bf16_pair(d, ad, bd, id_main, more);
+        umma_bf16_pair(d, ad + a_step, bd + b_step, id_main, 1);
+        umma_bf16_pair(d, ad + 2 * a_step, bd + 2 * b_step, id_main, 1);
+        umma_bf16_pair(d, ad + 3 * a_step, bd + 3 * b_step, id_main, 1);
       };
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
         const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
-        // accumulations of one length: the same steps of 16 each, no column to keep
-        const int regular = parts.part % 64 == 0 && group % parts.part == 0 && c.k0 % parts.part == 0 && c.k1 % parts.part == 0 ? parts.part >> 4 : 0;
-        if (!regular) parts.start(c.k0);
-        int k = c.k0, left = 0, todo = (c.k1 - c.k0 + 15) >> 4;  // column; steps of 16 of the accumulation under way, of the tile
-        for (int st = 0; st < n_st + c.lora; ++st) {
-          ok = mbar_wait_warp(full_bar(s), phase, abort_flag, &g_packed_error);
+        int st = 0, left = 0;
+        // accumulations of one length and of whole pairs of stages: nothing to keep but how many pairs are left
+        const int len = BACK ? c.k1 - c.k0 : parts.part;
+        const bool regular = BACK || (group % len == 0 && c.k0 % len == 0 && c.k1 % len == 0);
+        if (regular && len % (2 * PT_BK) == 0 && s % 2 == 0) {
+          uint32_t d = 0, more = 0;
+          for (; st < n_st; st += 2) {
+            if (left == 0) {
+              ok = acc_free();
+              left = len / (2 * PT_BK);
+              d = tmem_base + (acc_it & 1u) * 256u;
+              more = 0;
+            }
+            const uint32_t at = s * (PT_STAGE_BYTES >> 4);
+            ok = ok && wait(full_bar(s), phase);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (!ok) break;
+            if (one) {
+              four(d, a_main + at, b_main + at, more);
+              umma_commit_pair(empty_bar(s));
+            }
+            ok = wait(full_bar(s + 1), phase);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (!ok) break;
+            --left;
+            if (one) {
+              four(d, a_main + at + (PT_STAGE_BYTES >> 4), b_main + at + (PT_STAGE_BYTES >> 4), 1);
+              umma_commit_pair(empty_bar(s + 1));
+              if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
+            }
+            more = 1;
+            if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
+            s += 2;
+            if (s == STAGES) s = 0, phase ^= 1u;
+          }
+        }
+        int k = c.k0, todo = (c.k1 - c.k0 + 15) >> 4;  // column; steps of 16 left of the tile
+        if (st < n_st) parts.start(c.k0);
+        for (; st < n_st + c.lora && ok; ++st) {
+          ok = wait(full_bar(s), phase);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = s * (PT_STAGE_BYTES >> 4);
           const uint64_t bd = b_main + at;
           if (st < n_st) {
             const uint64_t ad = a_main + at;
-            uint32_t more = 1;
-            if (left == 0) {
-              ok = acc_free();
-              if (!ok) break;
-              left = regular;
-              if (!regular) {
-                left = (min(parts.end, c.k1) - k + 15) >> 4;
+            const int steps = min(4, todo);
+            todo -= steps;
+            for (int kk = 0; kk < steps; ++kk) {
+              uint32_t more = 1;
+              if (left == 0) {
+                ok = acc_free();
+                if (!ok) break;
+                left = BACK ? todo + steps - kk : (min(parts.end, c.k1) - k + 15) >> 4;
                 parts.next();
+                more = 0;
               }
-              more = 0;
-            }
-            if (left >= 4 && todo >= 4) {  // the whole stage in one accumulation
-              const uint32_t d = tmem_base + (acc_it & 1u) * 256u;
-              left -= 4;
+              --left;
               if (one) {
-                umma_bf16_pair(d, ad, bd, id_main, more);
-                umma_bf16_pair(d, ad + a_step, bd + b_step, id_main, 1);
-                umma_bf16_pair(d, ad + 2 * a_step, bd + 2 * b_step, id_main, 1);
-                umma_bf16_pair(d, ad + 3 * a_step, bd + 3 * b_step, id_main, 1);
-                umma_commit_pair(empty_bar(s));
-                if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
+                umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, ad + kk * a_step, bd + kk * b_step, id_main, more);
+                if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
               }
-              __syncwarp();
-              todo -= 4, k += 64;
-              if (left == 0) ++acc_it;
-            } else {
-              const int steps = min(4, todo);
-              todo -= steps;
-              for (int kk = 0; kk < steps; ++kk) {
-                if (left == 0) {
-                  ok = acc_free();
-                  if (!ok) break;
-                  left = (min(parts.end, c.k1) - k + 15) >> 4;
-                  parts.next();
-                  more = 0;
-                }
-                --left;
-                if (one) {
-                  umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, ad + kk * a_step, bd + kk * b_step, id_main, more);
-                  if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
-                }
-                __syncwarp();
-                more = 1;
-                k += 16;
-                if (left == 0) ++acc_it;
-              }
-              if (!ok) break;
-              if (one) umma_commit_pair(empty_bar(s));
-              __syncwarp();
+              k += 16;
+              if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
             }
+            if (!ok) break;
+            if (one) umma_commit_pair(empty_bar(s));
           } else {
-            if (st == n_st) {
+            if (!BACK && st == n_st) {  // forward, an accumulation of their own: no scale applies to them
               ok = acc_free();
               if (!ok) break;
             }
@@ -321,11 +350,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
             if (one) {
 #pragma unroll
               for (int kk = 0; kk < PT_BK / 16; ++kk)
-                umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, a_lora + at + kk * l_step, bd + kk * b_step, id_lora, st == n_st && kk == 0 ? 0u : 1u);
+                umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, a_lora + at + kk * l_step, bd + kk * b_step, id_lora,
+                               !BACK && st == n_st && kk == 0 ? 0u : 1u);
               umma_commit_pair(empty_bar(s));
               if (last) umma_commit_pair(accf_bar(acc_it & 1u));
             }
-            __syncwarp();
             if (last) ++acc_it;
           }
           if (++s == STAGES) s = 0, phase ^= 1u;
@@ -342,26 +371,38 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
         const int n_u = BACK ? (c.k1 - c.k0 + 63) / 64 : (c.k1 - c.k0 + 127) / 128;
+        int r = BACK ? c.k0 : c.m0, j = BACK ? c.m0 : c.k0, g = (j >> 5) / G, left = (g + 1) * G - (j >> 5);
+        const unsigned* zt = p.zt + ((long long)g * p.rows_pad + r) * (BACK ? 2 : 1);  // of the unit's first run
         for (int u = 0; u < n_u; ++u) {
           ok = mbar_wait(raw_empty(s), phase, abort_flag, &g_packed_error);
           if (!ok) break;
-          const uint32_t dst = raw_base + s * Ring::PAD;
-          const int r = BACK ? c.k0 + 64 * u : c.m0, j = BACK ? c.m0 : c.k0 + 128 * u;
-          mbar_expect_tx(raw_full(s), bytes);
-          tma_load_2d(dst, &wmap, (j >> 5) * BITS, r, raw_full(s));
-          for (int h = 0; h < n_sz; ++h) {
-            const long long at = (long long)(min((j >> 5) + h, last) / G) * p.rows_pad + r;
-            bulk_load(dst + Ring::Z + h * Ring::ROWS * 4, p.zt + at, Ring::ROWS * 4, raw_full(s));
-            if (BACK) bulk_load(dst + Ring::S + h * Ring::ROWS * 4, p.st + at, Ring::ROWS * 4, raw_full(s));
+          const uint32_t dst = raw_base + s * Ring::PAD, bar = raw_full(s);
+          mbar_expect_tx(bar, bytes);
+          tma_load_2d(dst, &wmap, (j >> 5) * BITS, r, bar);
+          if (n_sz == 1) {
+            bulk_load(dst + Ring::Z, zt, Ring::ROWS * (BACK ? 8 : 4), bar);
+          } else {
+            for (int h = 0; h < 4; ++h) {
+              const long long at = (long long)(min((j >> 5) + h, last) / G) * p.rows_pad + r;
+              bulk_load(dst + Ring::Z + h * Ring::ROWS * (BACK ? 8 : 4), p.zt + at * (BACK ? 2 : 1), Ring::ROWS * (BACK ? 8 : 4), bar);
+            }
+          }
+          if (BACK) {
+            r += 64;
+            zt += 128;
+          } else {
+            j += 128;
+            left -= 4;
+            if (left == 0) left = G, zt += p.rows_pad;
           }
           if (++s == Ring::STAGES) s = 0, phase ^= 1u;
         }
       }
     }
-  } else if (warp < 12) {
+  } else if (warp < R::EPI0) {
     // ---------------- decode: operand A of this CTA ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    const int tid = (threadIdx.x - 128) & 127, turn = (warp - 4) >> 2;  // two warpgroups take turns at the stages
+    if (!BACK) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    const int tid = (threadIdx.x - 128) & 127, turn = (warp - 4) >> 2;  // the warpgroups take turns at the units
     // forward: thread = tile row (a weight row), 64 contraction columns of a stage; backward: 64 weight rows x two halves
     const int my_row = BACK ? tid & 63 : tid;
     const uint32_t row_off = BACK ? (uint32_t)(tid >> 6) * 8192u + (uint32_t)my_row * 128u : (uint32_t)my_row * 128u;
@@ -375,7 +416,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
       for (int st = 0; st < n_st && ok; st += PER, ++unit) {
         const int here = min(PER, n_st - st);
-        if ((int)(unit & 1u) != turn) {
+        if ((int)(unit % R::DECODE) != turn) {
           it += here;
           continue;
         }
@@ -405,12 +446,13 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int o = (one_sz ? 0 : 2 * half + h) * Ring::ROWS * 4 + my_row * 4;
-            z[h] = *reinterpret_cast<const unsigned*>(q + Ring::Z + o);
-            if (BACK) {
-              const float v = *reinterpret_cast<const float*>(q + Ring::S + o);
-              sc[h][0] = bf2(__float2bfloat162_rn(v));
-              sc[h][1] = bf2(__float2bfloat162_rn(v - __uint_as_float(sc[h][0] << 16)));
+            const int o = (one_sz ? 0 : 2 * half + h) * Ring::ROWS + my_row;
+            if constexpr (BACK) {
+              const uint2 v = reinterpret_cast<const uint2*>(q + Ring::Z)[o];
+              z[h] = v.x;
+              sc[h][0] = __byte_perm(v.y, 0, 0x3232), sc[h][1] = __byte_perm(v.y, 0, 0x1010);
+            } else {
+              z[h] = reinterpret_cast<const unsigned*>(q + Ring::Z)[o];
             }
           }
           if (i == here - 1) {
@@ -430,7 +472,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
       // the adapters (where the sum is not split): four slots a stage, slot = (run, 16 of the rank, piece)
       const int n_slots = c.n_runs * nb * 2;
       for (int st = 0; st < c.lora && ok; ++st, ++it) {
-        if ((int)(it & 1u) != turn) continue;
+        if ((int)(it % R::DECODE) != turn) continue;
         const int s = it % STAGES;
         const uint32_t sa = base + s * PT_STAGE_BYTES, sb = sa + PT_A_BYTES;
         {
@@ -499,62 +541,92 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_tc(const __grid_consta
     }
   } else {
     // ---------------- epilogue: 128 columns (TMEM lanes), half of the tokens each ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
-    const int q = warp & 3, hf = (warp - 12) >> 2;
+    if (!BACK) asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    const int q = warp & 3, hf = BACK ? 0 : (warp - R::EPI0) >> 2, my_n = BACK ? p.n_tile : half_n;
     Parts parts(group);
     uint32_t acc_it = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile c = tile_of(t);
       const int col = c.m0 + q * 32 + lane;
-      float run[128];
-#pragma unroll
-      for (int i = 0; i < 128; ++i) run[i] = 0.0f;
-      parts.start(c.k0);
-      int k = c.k0;
-      bool lora = false;
-      while (ok) {
-        if (k >= c.k1) {
-          if (lora || c.lora == 0) break;
-          lora = true;
-        }
-        float s = 1.0f;
-        if (!BACK && !lora) s = __ldg(p.st + (long long)parts.g * p.rows_pad + col);
-        const uint32_t b = acc_it & 1u;
-        ok = mbar_wait_warp(accf_bar(b), (acc_it >> 1) & 1u, abort_flag, &g_packed_error);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256u + (uint32_t)(hf * half_n);
-#pragma unroll
-        for (int ch = 0; ch < 8; ++ch) {
-          if (16 * ch >= half_n) break;
-          uint32_t r[16];
-          tmem_ld_32x16(taddr + ch * 16, r);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-          for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
-        }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive_remote_relaxed(map_to_rank(acce_bar(b), 0));
-        ++acc_it;
-        if (!lora) k = parts.end, parts.next();
-      }
-      if (!ok) break;
-      const int tok0 = c.t0 + hf * half_n, n = min(half_n, p.n_tok - tok0);  // this warp's tokens
-      if (col >= p.n_cols || n <= 0) continue;
+      const int tok0 = c.t0 + hf * half_n, n = min(my_n, p.n_tok - tok0);  // this warp's tokens
+      const bool store = col < p.n_cols && n > 0;
       const long long at = (long long)tok0 * p.n_cols + col;
       float* fo = p.part + (long long)c.split * p.n_tok * p.n_cols + at;
       __nv_bfloat16* bo = p.out + at;
-      if (p.splits > 1) {
+      const uint32_t tmem_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(hf * half_n);
+      auto acc_full = [&]() {
+        ok = mbar_wait_warp(accf_bar(acc_it & 1u), (acc_it >> 1) & 1u, abort_flag, &g_packed_error);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        return ok;
+      };
+      auto acc_read = [&]() {
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote_relaxed(map_to_rank(acce_bar(acc_it & 1u), 0));
+        ++acc_it;
+      };
+      if constexpr (BACK) {
+        if (!acc_full()) break;
+        const uint32_t taddr = tmem_row + (acc_it & 1u) * 256u;
+        for (int ch = 0; 16 * ch < my_n; ++ch) {
+          uint32_t r[16];
+          tmem_ld_32x16(taddr + ch * 16, r);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (!store) continue;
+          if (p.splits > 1) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-          if (i < n) fo[i * p.n_cols] = run[i];
+            for (int i = 0; i < 16; ++i)
+              if (16 * ch + i < n) fo[(16 * ch + i) * p.n_cols] = __uint_as_float(r[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (16 * ch + i < n) bo[(16 * ch + i) * p.n_cols] = __float2bfloat16(__uint_as_float(r[i]));
+          }
+        }
+        acc_read();
       } else {
+        uint64_t run[64];  // two floats each: fma.rn.f32x2 halves the additions' instructions
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-          if (i < n) bo[i * p.n_cols] = __float2bfloat16(run[i]);
+        for (int i = 0; i < 64; ++i) run[i] = 0;
+        parts.start(c.k0);
+        int k = c.k0;
+        bool lora = false;
+        while (true) {
+          if (k >= c.k1) {
+            if (lora || c.lora == 0) break;
+            lora = true;
+          }
+          float s = 1.0f;
+          if (!lora) s = __ldg(p.st + (long long)parts.g * p.rows_pad + col);
+          if (!acc_full()) break;
+          const uint32_t taddr = tmem_row + (acc_it & 1u) * 256u;
+#pragma unroll
+          for (int ch = 0; ch < 8; ++ch) {
+            if (16 * ch >= half_n) break;
+            uint32_t r[16];
+            tmem_ld_32x16(taddr + ch * 16, r);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fma_two(run[8 * ch + i], r[2 * i], r[2 * i + 1], s);
+          }
+          acc_read();
+          if (!lora) k = parts.end, parts.next();
+        }
+        if (!ok) break;
+        if (store) {
+          if (p.splits > 1) {
+#pragma unroll
+            for (int i = 0; i < 128; ++i)
+              if (i < n) fo[i * p.n_cols] = __uint_as_float((unsigned)(run[i >> 1] >> (32 * (i & 1))));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 128; ++i)
+              if (i < n) bo[i * p.n_cols] = __float2bfloat16(__uint_as_float((unsigned)(run[i >> 1] >> (32 * (i & 1)))));
+          }
+        }
       }
+      if (!store) continue;
       // what is not finite in the adapters' rows, to the tokens that it belongs to: whatever finite value was stored there stops
       // being one.  (The flag was set before the adapters' last stage was handed over, hence before its accumulation was complete.)
       if (c.lora && *odd_flag)
@@ -592,13 +664,13 @@ tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& xmap, const CUt
   if (!configured[dev]) {
     cudaFuncAttributes at;
     TB_CUDA_CHECK(cudaFuncGetAttributes(&at, k_packed_tc<BITS, BACK>));
-    if (at.numRegs != 96) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 96 registers a thread has
+    if (!BACK && at.numRegs != 96) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 96 registers a thread has
     TB_CUDA_CHECK(cudaFuncSetAttribute(k_packed_tc<BITS, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PT_SMEM));
     configured[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
-  cfg.blockDim = dim3(PT_THREADS);
+  cfg.blockDim = dim3(Roles<BACK>::THREADS);
   cfg.dynamicSmemBytes = PT_SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
