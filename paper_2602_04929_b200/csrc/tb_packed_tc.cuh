@@ -133,16 +133,6 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
   return *reinterpret_cast<const unsigned short*>(&lo);
 }
 
-// both halves of c += a pair times s
-__device__ __forceinline__ void fma_two(uint64_t& c, uint32_t a0, uint32_t a1, float s) {
-  asm("{\n\t.reg .b64 a, b;\n\t"
-      "mov.b64 a, {%1, %2};\n\t"
-      "mov.b64 b, {%3, %3};\n\t"
-      "fma.rn.f32x2 %0, a, b, %0;\n\t}"
-      : "+l"(c)
-      : "r"(a0), "r"(a1), "f"(s));
-}
-
 template <bool BACK>
 struct Roles {
   enum { DECODE = BACK ? 4 : 2, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
@@ -586,9 +576,9 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
         }
         acc_read();
       } else {
-        uint64_t run[64];  // two floats each: fma.rn.f32x2 halves the additions' instructions
+        float run[128];
 #pragma unroll
-        for (int i = 0; i < 64; ++i) run[i] = 0;
+        for (int i = 0; i < 128; ++i) run[i] = 0.0f;
         parts.start(c.k0);
         int k = c.k0;
         bool lora = false;
@@ -608,7 +598,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             tmem_ld_32x16(taddr + ch * 16, r);
             asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 8; ++i) fma_two(run[8 * ch + i], r[2 * i], r[2 * i + 1], s);
+            for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
           }
           acc_read();
           if (!lora) k = parts.end, parts.next();
@@ -618,11 +608,11 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           if (p.splits > 1) {
 #pragma unroll
             for (int i = 0; i < 128; ++i)
-              if (i < n) fo[i * p.n_cols] = __uint_as_float((unsigned)(run[i >> 1] >> (32 * (i & 1))));
+              if (i < n) fo[i * p.n_cols] = run[i];
           } else {
 #pragma unroll
             for (int i = 0; i < 128; ++i)
-              if (i < n) bo[i * p.n_cols] = __float2bfloat16(__uint_as_float((unsigned)(run[i >> 1] >> (32 * (i & 1)))));
+              if (i < n) bo[i * p.n_cols] = __float2bfloat16(run[i]);
           }
         }
       }
