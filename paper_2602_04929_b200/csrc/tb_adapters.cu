@@ -17,19 +17,20 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
+static __device__ int g_grad_error = 0;
+
 // ------------------------------------------------------------------------------------------ x A_i^T
 //
-// A CTA has TT tokens (64, or 16 where there are few), one of the adapters that they have, up to 64 of its rank and, as one of a
-// cluster, a share of the contraction; its warps split the tokens into MT x 16 and the contraction further.  Operands go from
-// global memory straight into fragments: a lane loads 16 bytes of a row, eight neighbouring columns, and which columns a fragment
+// For few tokens, on mma.sync: a CTA has 16 tokens, one of the adapters that they have, up to 64 of its rank and, as one of a
+// cluster, a share of the contraction, which its warps split further.  Operands go from global memory straight into fragments: a lane loads 16 bytes of a row, eight neighbouring columns, and which columns a fragment
 // calls k = 0 .. 15 does not matter as long as both operands agree.  Rows of other adapters are not read.  The warps' and the CTAs'
 // sums are added in a fixed order.
 
-template <int MT, int NT>
+template <int NT>
 __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat16* __restrict__ in, const __nv_bfloat16* __restrict__ M,
                                                      int n_tok, int width, float* __restrict__ low) {
-  constexpr int TT = MT == 2 ? 64 : 16, WT = TT / (16 * MT), KG = 8 / WT, R = 8 * NT, PITCH = R + 1;
-  __shared__ int own[TT], pick[3];
+  constexpr int TT = 16, KG = 8, R = 8 * NT, PITCH = R + 1;
+  __shared__ int own[TT], pick;
   __shared__ float sum[TT * PITCH];
   uint32_t rank, cs;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -38,21 +39,14 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
   const int t0 = (blockIdx.x / cs) * TT, r0 = blockIdx.z * 64;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x < TT) own[threadIdx.x] = t0 + (int)threadIdx.x < n_tok ? adapter_of(ad, t0 + threadIdx.x) : -2;
-  if (threadIdx.x == 0) pick[0] = -1, pick[1] = 0;
+  if (threadIdx.x == 0) pick = -1;
   __syncthreads();
   // the blockIdx.y-th adapter among the tile's, by its first token
   if (threadIdx.x < 32) {
-    int before = 0;
-#pragma unroll
-    for (int b = 0; b < TT; b += 32) {
-      const int i = b + lane;
-      bool first = i < TT && own[i < TT ? i : 0] >= 0;
-      for (int k = 0; first && k < i; ++k) first = own[k] != own[i];
-      const unsigned m = __ballot_sync(0xffffffffu, first);
-      const int at = before + __popc(m & ((1u << lane) - 1u));
-      if (first && at == (int)blockIdx.y) pick[0] = own[i];
-      before += __popc(m);
-    }
+    bool first = lane < TT && own[lane & (TT - 1)] >= 0;
+    for (int k = 0; first && k < lane; ++k) first = own[k] != own[lane];
+    const unsigned m = __ballot_sync(0xffffffffu, first);
+    if (first && __popc(m & ((1u << lane) - 1u)) == (int)blockIdx.y) pick = own[lane];
   }
   __syncthreads();
   if (blockIdx.y == 0 && rank == 0)  // tokens without an adapter
@@ -60,50 +54,46 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
       const int t = e / R, r = r0 + e % R;
       if (own[t] == -1 && r < ad.rank) low[(long long)(t0 + t) * ad.rank + r] = 0.0f;
     }
-  const int id = pick[0];
+  const int id = pick;
   if (id < 0) return;  // the same in every CTA of the cluster
-  const int g = lane >> 2, q = lane & 3, tg = warp % WT, kg = warp / WT;
-  const __nv_bfloat16* xr[2 * MT];
+  const int g = lane >> 2, q = lane & 3;
+  const __nv_bfloat16* xr[2];
   const __nv_bfloat16* mr[NT];
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {
-    const int t = tg * 16 * MT + 8 * i + g;
+  for (int i = 0; i < 2; ++i) {
+    const int t = 8 * i + g;
     xr[i] = own[t] == id ? in + (long long)(t0 + t) * width : nullptr;
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n) mr[n] = r0 + 8 * n + g < ad.rank ? M + ((long long)id * ad.rank + r0 + 8 * n + g) * width : nullptr;
-  float acc[MT][NT][4] = {};
+  float acc[NT][4] = {};
   const int steps = (width + 31) / 32, per = (steps + (int)cs * KG - 1) / ((int)cs * KG);
-  const int s0 = ((int)rank * KG + kg) * per, s1 = min(steps, s0 + per);
+  const int s0 = ((int)rank * KG + warp) * per, s1 = min(steps, s0 + per);
 #pragma unroll 4
   for (int s = s0; s < s1; ++s) {
     const int k = 32 * s + 8 * q;
     const bool in_k = k < width;
-    uint4 x[2 * MT], m[NT];
+    uint4 x[2], m[NT];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) x[i] = in_k && xr[i] ? __ldg(reinterpret_cast<const uint4*>(xr[i] + k)) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < 2; ++i) x[i] = in_k && xr[i] ? __ldg(reinterpret_cast<const uint4*>(xr[i] + k)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int n = 0; n < NT; ++n) m[n] = in_k && mr[n] ? __ldg(reinterpret_cast<const uint4*>(mr[n] + k)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma_bf16(acc[i][n], x[2 * i].x, x[2 * i + 1].x, x[2 * i].y, x[2 * i + 1].y, m[n].x, m[n].y);
-        mma_bf16(acc[i][n], x[2 * i].z, x[2 * i + 1].z, x[2 * i].w, x[2 * i + 1].w, m[n].z, m[n].w);
-      }
+    for (int n = 0; n < NT; ++n) {
+      mma_bf16(acc[n], x[0].x, x[1].x, x[0].y, x[1].y, m[n].x, m[n].y);
+      mma_bf16(acc[n], x[0].z, x[1].z, x[0].w, x[1].w, m[n].z, m[n].w);
+    }
   }
   // the warps along the contraction, one after the other
   for (int k = 0; k < KG; ++k) {
-    if (kg == k) {
+    if (warp == k) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float* o = sum + (tg * 16 * MT + 16 * i + g + 8 * (c >> 1)) * PITCH + 8 * n + 2 * q + (c & 1);
-            *o = k ? *o + acc[i][n][c] : acc[i][n][c];
-          }
+        for (int c = 0; c < 4; ++c) {
+          float* o = sum + (g + 8 * (c >> 1)) * PITCH + 8 * n + 2 * q + (c & 1);
+          *o = k ? *o + acc[n][c] : acc[n][c];
+        }
     }
     __syncthreads();
   }
@@ -122,10 +112,10 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
   if (cs > 1) cluster_barrier();  // nobody leaves while its sums are read
 }
 
-template <int MT, int NT>
+template <int NT>
 static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
                             cudaStream_t st) {
-  constexpr int TT = MT == 2 ? 64 : 16;
+  constexpr int TT = 16;
   const int tiles = (n_tok + TT - 1) / TT, zs = (ad.rank + 63) / 64;
   const int ys = min(TT, min(ad.n_req, ad.n));
   // clusters along the contraction until about two CTAs an SM: adapters are counted as if the requests were spread over the tiles
@@ -144,7 +134,208 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low<MT, NT>, ad, in, M, n_tok, width, low));
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low<NT>, ad, in, M, n_tok, width, low));
+  TB_LAUNCH_CHECK();
+  return TB_OK;
+}
+
+// The same for many tokens, on tcgen05: 128 tokens are the rows M of the tile, the rank its columns N, both operands by TMA as they
+// are stored (K-major).  x so is read once, at HBM's rate, and an adapter once for 128 tokens.  A tile's adapters (AL_COLS / N of
+// them, more in further CTAs) are gone through one after the other, each into columns of its own; rows of other adapters are computed and dropped.
+// CTAs of a cluster share the contraction; an accumulation ends after 2048 columns where tensor memory has room for more of them.
+
+enum { LOW_TC_WORK = 65536 };  // tokens x rank
+enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_PART = 2048, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
+
+struct LowTc {
+  Adapt ad;
+  float* low;
+  int n_tok, width, n, stages, per, part, n_parts;  // n: the rank rounded up to 16; per: contraction columns of a CTA
+};
+
+__global__ void __launch_bounds__(AL_THREADS, 1)
+    k_adapter_low_tc(const __grid_constant__ LowTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap mmap) {
+  extern __shared__ unsigned char al_raw[];
+  __shared__ __align__(8) unsigned long long bars[2 * 16 + 1];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int gave_up, own[AL_TOK], cand[AL_TOK], firsts[4], n_ids;
+  const uint32_t base = (smem_u32(al_raw) + 1023u) & ~1023u;
+  float* sums = reinterpret_cast<float*>(al_raw + (base - smem_u32(al_raw)));  // after the last stage: [128][n + 1]
+  const uint32_t bar0 = smem_u32(bars), done_bar = bar0 + 8u * 32;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (16 + s); };
+  uint32_t rank, cs;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
+  const int t0 = (blockIdx.x / cs) * AL_TOK, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(done_bar, 1);
+    gave_up = 0;
+    mbar_fence_init();
+  }
+  if (tid < AL_TOK) own[tid] = t0 + tid < p.n_tok ? adapter_of(p.ad, t0 + tid) : -2;
+  __syncthreads();
+  {
+    const bool first = tid < AL_TOK && own[tid] >= 0 && (tid == 0 || own[tid - 1] != own[tid]);
+    const unsigned m = __ballot_sync(0xffffffffu, first);
+    if (warp < 4 && lane == 0) firsts[warp] = __popc(m);
+    __syncthreads();
+    int at = __popc(m & ((1u << lane) - 1u));
+    for (int k = 0; k < min(warp, 4); ++k) at += firsts[k];
+    if (first) cand[at] = own[tid];
+    __syncthreads();
+    if (tid == 0) {  // each adapter once, in the order of their first tokens
+      const int all = firsts[0] + firsts[1] + firsts[2] + firsts[3];
+      int n = 0;
+      for (int i = 0; i < all; ++i) {
+        int k = 0;
+        while (k < n && cand[k] != cand[i]) ++k;
+        if (k == n) cand[n++] = cand[i];
+      }
+      n_ids = n;
+    }
+    __syncthreads();
+  }
+  const int room = AL_COLS / (p.n * p.n_parts), id0 = (int)blockIdx.y * room, ids = min(room, n_ids - id0);
+  if (blockIdx.y == 0 && rank == 0)  // tokens without an adapter
+    for (int e = tid; e < AL_TOK * p.ad.rank; e += AL_THREADS)
+      if (own[e / p.ad.rank] == -1) p.low[(long long)t0 * p.ad.rank + e] = 0.0f;
+  if (ids <= 0) return;  // the same in every CTA of the cluster
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((uint32_t)AL_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+  const int stage_bytes = AL_TOK * 128 + p.n * 128;  // a multiple of 1024: n is one of 16, hence of 8 rows of 128 bytes
+  const int k0 = (int)rank * p.per, k1 = min(p.width, k0 + p.per), n_st = k1 > k0 ? (k1 - k0 + AL_BK - 1) / AL_BK : 0;
+  if (warp == 4 && lane == 0) {
+    int s = 0;
+    uint32_t phase = 1;
+    bool ok = true;
+    for (int a = 0; a < ids && ok; ++a)
+      for (int st = 0; st < n_st; ++st) {
+        ok = mbar_wait(empty_bar(s), phase, &gave_up, &g_grad_error);
+        if (!ok) break;
+        const uint32_t dst = base + s * stage_bytes;
+        mbar_expect_tx(full_bar(s), stage_bytes);
+        tma_load_2d(dst, &xmap, k0 + st * AL_BK, t0, full_bar(s));
+        tma_load_2d(dst + AL_TOK * 128, &mmap, k0 + st * AL_BK, cand[id0 + a] * p.ad.rank, full_bar(s));
+        if (++s == p.stages) s = 0, phase ^= 1u;
+      }
+  } else if (warp == 5) {
+    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(p.n >> 3) << 17) | (8u << 24);
+    const bool one = elect_one();
+    const uint64_t desc = smem_desc_k(base, 16) & ~((uint64_t)0x3fff << 32) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)2 << 61);
+    int s = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int a = 0; a < ids && ok; ++a) {
+      int in_part = 0, part = 0;
+      for (int st = 0; st < n_st; ++st) {
+        ok = mbar_wait(full_bar(s), phase, &gave_up, &g_grad_error);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (one) {
+          const uint64_t x = desc + (uint64_t)(s * (stage_bytes >> 4)), m = x + (AL_TOK * 128 >> 4);
+          const uint32_t d = tmem + (uint32_t)((a * p.n_parts + part) * p.n);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) umma_bf16(d, x + 2 * kk, m + 2 * kk, idesc, in_part > 0 || kk > 0 ? 1u : 0u);
+          umma_commit(empty_bar(s));
+        }
+        if (++in_part == p.part) in_part = 0, ++part;
+        if (++s == p.stages) s = 0, phase ^= 1u;
+      }
+    }
+    if (one) umma_commit(done_bar);
+  }
+  __syncthreads();
+  bool ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, &gave_up, &g_grad_error));
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t mine = smem_u32(sums);
+  const int pitch = p.n + 1, parts_here = (n_st + p.part - 1) / p.part;
+  for (int a = 0; a < ids; ++a) {
+    if (warp < 4)
+      for (int c = 0; c < p.n; c += 8) {
+        float v[8] = {};
+        for (int part = 0; part < parts_here && ok; ++part) {
+          uint32_t r[8];
+          tmem_ld_32x8(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)((a * p.n_parts + part) * p.n + c), r);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(r[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[tid * pitch + c + i] = v[i];
+      }
+    __syncthreads();
+    if (cs > 1) cluster_barrier();
+    const int id = cand[id0 + a];
+    for (int e = tid + AL_THREADS * (int)rank; e < AL_TOK * p.ad.rank; e += AL_THREADS * (int)cs) {
+      const int t = e / p.ad.rank, r = e - t * p.ad.rank;
+      if (own[t] != id) continue;
+      float v = 0.0f;
+      for (uint32_t k = 0; k < cs; ++k) {
+        const float u = cs > 1 ? ld_cluster(map_to_rank(mine + 4u * (t * pitch + r), k)) : sums[t * pitch + r];
+        v = k ? v + u : u;
+      }
+      p.low[(long long)t0 * p.ad.rank + e] = v;
+    }
+    if (cs > 1)
+      cluster_barrier();
+    else
+      __syncthreads();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)AL_COLS) : "memory");
+}
+
+static tb_status launch_low_tc(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, cudaStream_t st) {
+  static bool configured[64] = {false};
+  int dev = 0;
+  TB_CUDA_CHECK(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return TB_ERR_CUDA;
+  if (!configured[dev]) {
+    TB_CUDA_CHECK(cudaFuncSetAttribute(k_adapter_low_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, AL_ROOM + 1024));
+    configured[dev] = true;
+  }
+  const int tiles = (n_tok + AL_TOK - 1) / AL_TOK, sms = sm_count() > 0 ? sm_count() : 148;
+  int cs = 1;  // CTAs along the contraction, up to one an SM
+  while (cs < 8 && tiles * cs * 2 <= sms && width / (2 * cs) >= 256) cs *= 2;
+  LowTc p;
+  p.ad = ad, p.low = low, p.n_tok = n_tok, p.width = width;
+  p.n = (ad.rank + 15) / 16 * 16;
+  p.per = ((width + cs - 1) / cs + AL_BK - 1) / AL_BK * AL_BK;
+  p.n_parts = min((p.per + AL_PART - 1) / AL_PART, AL_COLS / p.n);
+  p.part = ((p.per / AL_BK) + p.n_parts - 1) / p.n_parts;
+  const int stage = AL_TOK * 128 + p.n * 128;
+  p.stages = min(12, AL_ROOM / stage);
+  const int ys = (min(AL_TOK, min(ad.n_req, ad.n)) + AL_COLS / (p.n * p.n_parts) - 1) / (AL_COLS / (p.n * p.n_parts));
+  CUtensorMap xmap, mmap;
+  TB_TRY(make_map_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, in, (unsigned long long)width, (unsigned long long)n_tok, AL_BK, AL_TOK,
+                     CU_TENSOR_MAP_SWIZZLE_128B));
+  TB_TRY(make_map_2d(&mmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, M, (unsigned long long)width, (unsigned long long)ad.n * ad.rank, AL_BK, p.n,
+                     CU_TENSOR_MAP_SWIZZLE_128B));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * cs), (unsigned)ys);
+  cfg.blockDim = dim3(AL_THREADS);
+  cfg.dynamicSmemBytes = AL_ROOM + 1024;  // no second CTA that would wait for tensor memory
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cs;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low_tc, p, xmap, mmap));
   TB_LAUNCH_CHECK();
   return TB_OK;
 }
@@ -152,13 +343,16 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
 // low [n_tok][rank] = in M_i^T for the adapter i of every token, zero for a token without one.
 tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
                            cudaStream_t st) {
-  // With 64 tokens a tile the adapters are read once for 64 tokens; with 16 there are more CTAs and less is computed for rows of
-  // other adapters.
-  const bool few = n_tok <= 512 || (long long)n_tok / ad.n_req < 48;
-  if (ad.rank <= 8) return few ? launch_low<1, 1>(ad, in, M, n_tok, width, low, st) : launch_low<2, 1>(ad, in, M, n_tok, width, low, st);
-  if (ad.rank <= 16) return few ? launch_low<1, 2>(ad, in, M, n_tok, width, low, st) : launch_low<2, 2>(ad, in, M, n_tok, width, low, st);
-  if (ad.rank <= 32) return few ? launch_low<1, 4>(ad, in, M, n_tok, width, low, st) : launch_low<2, 4>(ad, in, M, n_tok, width, low, st);
-  return few ? launch_low<1, 8>(ad, in, M, n_tok, width, low, st) : launch_low<2, 8>(ad, in, M, n_tok, width, low, st);
+  // Tiles of 16 tokens start sooner and compute less for rows of other adapters, but read an adapter once for every 16 tokens.
+  // Measured, tiles of 16 / tcgen05: 512 x 4096, rank 16, 6.4 / 8.6 us; 1999 x 4096, rank 32, 23 requests, 13.9 / 17.6 us;
+  // 1024 x 8192, rank 64, 29 / 20 us; 4099 x 8192, rank 64, 68 (tiles of 64) / 36 us.
+  if ((long long)n_tok * ad.rank < LOW_TC_WORK || (long long)n_tok / ad.n_req < 48) {
+    if (ad.rank <= 8) return launch_low<1>(ad, in, M, n_tok, width, low, st);
+    if (ad.rank <= 16) return launch_low<2>(ad, in, M, n_tok, width, low, st);
+    if (ad.rank <= 32) return launch_low<4>(ad, in, M, n_tok, width, low, st);
+    return launch_low<8>(ad, in, M, n_tok, width, low, st);
+  }
+  return launch_low_tc(ad, in, M, n_tok, width, low, st);
 }
 
 // ------------------------------------------------------------------------------------------ gradients
@@ -172,8 +366,6 @@ tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_
 // tokens; accumulations end after 2048 tokens; the CTAs' sums are added in a fixed order through distributed shared memory.
 
 enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 32, AG_THREADS = 288 };  // AG_PART: stages of an accumulation
-
-static __device__ int g_grad_error = 0;
 
 // RP: the rank, rounded up to 16, 32, 64 or 128.
 template <int RP>

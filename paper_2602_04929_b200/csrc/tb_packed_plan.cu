@@ -113,8 +113,9 @@ __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* 
   }
 }
 
-// Tile and splits by an estimate of the clocks: a stage costs what its MMAs take, 2 clocks a token of the tile, or its decoding,
-// a tile about 3000 clocks more, and splits cost writing and adding their float sums.
+// Tile and splits by an estimate of the clocks, fitted to sweeps of both (64 to 1999 tokens, widths of 1024 to 8192): a stage of 64
+// columns costs its decoding, whatever the tile, and a little for every token, a tile 1500 clocks and what its results take, and
+// splits cost writing and adding their float sums.
 TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
   TcPlan best = {};
   double best_cost = 0.0;
@@ -130,7 +131,7 @@ TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
       const long long tiles = (long long)m_tiles * t_tiles * splits;
       if (tiles > 0x3fffffff) continue;
       const double waves = (double)((tiles + pairs - 1) / pairs);
-      const double stage = 2.0 * n_tile > 200.0 ? 2.0 * n_tile : 200.0;
+      const double stage = 600.0 + 0.4 * n_tile;
       double cost = waves * (len / 64 * stage + 1500.0 + 6.0 * n_tile);
       if (splits > 1) cost += 4000.0 + 8.0 * splits * (double)n_tok * n_cols / 2500.0;
       if (best.n_tile == 0 || cost < best_cost) {
