@@ -504,7 +504,8 @@ def packed_weight(packed, scales, zeros, d_in: int, bits: int, quant_group: int 
             raise ValueError("scales and zeros must be [d_out][d_in / quant_group]")
     w = PackedWeight(packed.shape[0], d_in, bits, quant_group, _ptr(packed, torch.int32), _ptr(scales, torch.float32),
                      _ptr(zeros, torch.int32))
-    w.tensors = (packed, scales, zeros)
+    # what every call asks for, as plain attributes; scratch sizes by shape
+    w.tensors, w.widths, w.address, w.scratch = (packed, scales, zeros), (d_in, packed.shape[0]), ctypes.addressof(w), {}
     w.device = _one_device(w.tensors)
     return w
 
@@ -518,7 +519,8 @@ def adapters(A, B, scale, starts, ids) -> Adapters:
         raise ValueError("starts must have one entry more than ids")
     a = Adapters(A.shape[0], A.shape[1], ids.shape[0], _ptr(A), _ptr(B), _ptr(scale, torch.float32), _ptr(starts, torch.int32),
                  _ptr(ids, torch.int32))
-    a.tensors = (A, B, scale, starts, ids)
+    a.tensors, a.widths, a.address = (A, B, scale, starts, ids), (A.shape[2], B.shape[2]), ctypes.addressof(a)
+    a.shape, a.dtype = (A.shape[0], A.shape[1], ids.shape[0]), A.dtype
     a.device = _one_device(a.tensors)
     return a
 
@@ -531,47 +533,77 @@ def _one_device(tensors) -> int:
     return devices.pop()
 
 
-def _on_current(w, ad, *tensors) -> None:
-    """A call runs on the current device: everything it takes has to be there."""
-    cur = _current_device()
-    if w.device != cur or (ad is not None and ad.device != cur) or any(t is not None and t.device.index != cur for t in tensors):
-        raise ValueError("tensors must live on the current device")
+def _here(t, device: int, dtype) -> int:
+    """The address of a contiguous tensor on the current device."""
+    if t.get_device() != device:
+        raise ValueError("tensors must live on the current CUDA device (there is no CPU path)")
+    if t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous tensor of {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
-def _packed_call(w, ad, x, width, other):
-    """Checks of the activations and adapters of a call; (type, C pointers of w and ad)."""
-    if x.dim() != 2 or x.shape[1] != width:
-        raise ValueError(f"activations must be [n_tok][{width}]")
+_PACKED_TYPES = {torch.bfloat16: TB_BF16, torch.float32: TB_F32}
+
+
+def _packed_call(w, ad, x, side):
+    """Checks of a call's activations ([n_tok][widths[side]]) and adapters: (type, current device)."""
+    xt, device = _PACKED_TYPES.get(x.dtype), _current_device()
+    if xt is None:
+        raise ValueError("activations must be bfloat16 or float32")
+    if x.dim() != 2 or x.shape[1] != w.widths[side]:
+        raise ValueError(f"activations must be [n_tok][{w.widths[side]}]")
+    if w.device != device or (ad is not None and ad.device != device):
+        raise ValueError("tensors must live on the current CUDA device (there is no CPU path)")
     if ad is not None:
-        if ad.tensors[0].dtype != x.dtype:
+        if ad.dtype != x.dtype:
             raise ValueError("adapters must have the activations' dtype")
-        if (ad.tensors[0].shape[2], ad.tensors[1].shape[2]) != (w.d_in, w.d_out):
+        if ad.widths != w.widths:
             raise ValueError("adapters must be [n][rank][d_in] and [n][rank][d_out] of the projection")
-    return _xtype(x), ctypes.addressof(w), None if ad is None else ctypes.addressof(ad)
+    return xt, device
+
+
+def _scratch(query, w, ap, key, x, ws, device):
+    """(address, bytes, tensor) of a call's scratch: the caller's, or a new one of the size that its shapes need."""
+    if ws is not None:
+        if ws.get_device() != device or not ws.is_contiguous():
+            raise ValueError("the workspace must be contiguous and live on the current device")
+        return ws.data_ptr(), ws.numel() * ws.element_size(), ws
+    n = w.scratch.get(key)
+    if n is None:
+        if len(w.scratch) > 4096:
+            w.scratch.clear()
+        n = w.scratch[key] = query(w.address, ap, key[1], key[2])
+    if n == 0:
+        return None, 0, None
+    ws = x.new_empty(n, dtype=torch.uint8)
+    return ws.data_ptr(), n, ws
 
 
 def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=None, y=None, xa=None):
     """(y, xa): y = x Q^T, plus the adapters' share; xa [n_tok][rank] is x A^T of every token's adapter, which the backward
     pass takes (None without adapters)."""
-    xt, wp, ap = _packed_call(w, adapters, x, w.d_in, w.d_out)
-    n_tok = x.shape[0]
+    xt, device = _packed_call(w, adapters, x, 0)
+    n_tok, d_out = x.shape[0], w.widths[1]
     if y is None:
-        y = torch.empty((n_tok, w.d_out), dtype=x.dtype, device=x.device)
-    elif tuple(y.shape) != (n_tok, w.d_out):
+        y = x.new_empty((n_tok, d_out))
+    elif tuple(y.shape) != (n_tok, d_out):
         raise ValueError("y must be [n_tok][d_out]")
+    ap, xap, shape = None, None, None
     if adapters is None:
         xa = None
-    elif xa is None:
-        xa = torch.empty((n_tok, adapters.rank), dtype=torch.float32, device=x.device)
-    elif tuple(xa.shape) != (n_tok, adapters.rank):
-        raise ValueError("xa must be [n_tok][rank]")
-    _on_current(w, adapters, x, y, xa, ws)
+    else:
+        ap, shape = adapters.address, adapters.shape
+        if xa is None:
+            xa = x.new_empty((n_tok, shape[1]), dtype=torch.float32)
+        elif tuple(xa.shape) != (n_tok, shape[1]):
+            raise ValueError("xa must be [n_tok][rank]")
+        xap = _here(xa, device, torch.float32)
     lib = load()
-    if ws is None:
-        nbytes = lib.tb_packed_linear_workspace(wp, ap, xt, n_tok)
-        ws = _workspace(nbytes, x.device) if nbytes else None
-    _check(lib.tb_packed_linear(wp, ap, _ptr(x), xt, n_tok, _ptr(y, x.dtype), _ptr(xa, torch.float32, True),
-                                _ptr(ws, None, True), 0 if ws is None else ws.numel(), _stream()), "tb_packed_linear")
+    wsp, wsb, keep = _scratch(lib.tb_packed_linear_workspace, w, ap, (0, xt, n_tok, shape), x, ws, device)
+    status = lib.tb_packed_linear(w.address, ap, _here(x, device, x.dtype), xt, n_tok, _here(y, device, x.dtype), xap, wsp, wsb,
+                                  _stream())
+    if status:
+        raise TurboBoAError(status, "tb_packed_linear")
     return y, xa
 
 
@@ -579,54 +611,65 @@ def tb_packed_linear_backward(w: PackedWeight, dy, adapters: Adapters | None = N
                               want_dx: bool = True, ws=None):
     """(dx, dA, dB): gradients of tb_packed_linear.  The adapters' (float, None without adapters) need xa from the forward pass
     and its input, in full (x) or as `checkpoint`, the (codes, scales) of tb_checkpoint_pack."""
-    xt, wp, ap = _packed_call(w, adapters, dy, w.d_out, w.d_in)
-    n_tok, dev = dy.shape[0], dy.device
-    codes, cscales = checkpoint if checkpoint is not None else (None, None)
-    grads = adapters is not None and (x is not None or checkpoint is not None)
-    if grads:
-        if x is not None and (tuple(x.shape) != (n_tok, w.d_in) or x.dtype != dy.dtype):
-            raise ValueError("x must be [n_tok][d_in] of dy's dtype")
-        if codes is not None and (tuple(codes.shape) != (n_tok, w.d_in) or tuple(cscales.shape) != (n_tok, -(-w.d_in // 128))):
-            raise ValueError("checkpoint must be codes [n_tok][d_in] and scales [n_tok][d_in / 128]")
-        if xa is None or tuple(xa.shape) != (n_tok, adapters.rank):
-            raise ValueError("xa must be the forward pass's [n_tok][rank]")
-    dx = torch.empty((n_tok, w.d_in), dtype=dy.dtype, device=dev) if want_dx else None
-    dA = torch.empty(adapters.tensors[0].shape, dtype=torch.float32, device=dev) if grads else None
-    dB = torch.empty(adapters.tensors[1].shape, dtype=torch.float32, device=dev) if grads else None
-    _on_current(w, adapters, dy, x, codes, cscales, xa, ws)
+    xt, device = _packed_call(w, adapters, dy, 1)
+    n_tok, d_in = dy.shape[0], w.widths[0]
+    f32, xp, cp, sp, xap, dAp, dBp, dx, dA, dB, ap, shape = torch.float32, *([None] * 11)
+    if adapters is not None:
+        ap, shape = adapters.address, adapters.shape
+        if x is not None or checkpoint is not None:
+            if x is not None:
+                if tuple(x.shape) != (n_tok, d_in):
+                    raise ValueError("x must be [n_tok][d_in]")
+                xp = _here(x, device, dy.dtype)
+            if checkpoint is not None:
+                codes, cscales = checkpoint
+                if tuple(codes.shape) != (n_tok, d_in) or tuple(cscales.shape) != (n_tok, -(-d_in // 128)):
+                    raise ValueError("checkpoint must be codes [n_tok][d_in] and scales [n_tok][d_in / 128]")
+                cp, sp = _here(codes, device, torch.int8), _here(cscales, device, f32)
+            if xa is None or tuple(xa.shape) != (n_tok, shape[1]):
+                raise ValueError("xa must be the forward pass's [n_tok][rank]")
+            xap = _here(xa, device, f32)
+            dA = dy.new_empty((shape[0], shape[1], d_in), dtype=f32)
+            dB = dy.new_empty((shape[0], shape[1], w.widths[1]), dtype=f32)
+            dAp, dBp = dA.data_ptr(), dB.data_ptr()
+    if want_dx:
+        dx = dy.new_empty((n_tok, d_in))
     lib = load()
-    if ws is None:
-        nbytes = lib.tb_packed_linear_backward_workspace(wp, ap, xt, n_tok)
-        ws = _workspace(nbytes, dev) if nbytes else None
-    _check(lib.tb_packed_linear_backward(wp, ap, _ptr(dy), xt, n_tok, _ptr(x, dy.dtype, True), _ptr(codes, torch.int8, True),
-                                         _ptr(cscales, torch.float32, True), _ptr(xa, torch.float32, True),
-                                         _ptr(dx, None, True), _ptr(dA, None, True), _ptr(dB, None, True),
-                                         _ptr(ws, None, True), 0 if ws is None else ws.numel(), _stream()),
-           "tb_packed_linear_backward")
+    wsp, wsb, keep = _scratch(lib.tb_packed_linear_backward_workspace, w, ap, (1, xt, n_tok, shape), dy, ws, device)
+    status = lib.tb_packed_linear_backward(w.address, ap, _here(dy, device, dy.dtype), xt, n_tok, xp, cp, sp, xap,
+                                           dx.data_ptr() if want_dx else None, dAp, dBp, wsp, wsb, _stream())
+    if status:
+        raise TurboBoAError(status, "tb_packed_linear_backward")
     return dx, dA, dB
 
 
 def tb_checkpoint_pack(x):
     """x [n_tok][d] -> (codes int8 [n_tok][d], scales [n_tok][ceil(d / 128)]): activations in 8 bits."""
+    xt, device = _PACKED_TYPES.get(x.dtype), _current_device()
+    if xt is None or x.dim() != 2:
+        raise ValueError("activations must be [n_tok][d], bfloat16 or float32")
     n_tok, d = x.shape
-    codes = torch.empty((n_tok, d), dtype=torch.int8, device=x.device)
-    scales = torch.empty((n_tok, -(-d // 128)), dtype=torch.float32, device=x.device)
-    if x.device.index != _current_device():
-        raise ValueError("tensors must live on the current device")
-    _check(load().tb_checkpoint_pack(_ptr(x), _xtype(x), n_tok, d, _ptr(codes), _ptr(scales), _stream()), "tb_checkpoint_pack")
+    codes = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
+    scales = x.new_empty((n_tok, -(-d // 128)), dtype=torch.float32)
+    status = load().tb_checkpoint_pack(_here(x, device, x.dtype), xt, n_tok, d, codes.data_ptr(), scales.data_ptr(), _stream())
+    if status:
+        raise TurboBoAError(status, "tb_checkpoint_pack")
     return codes, scales
 
 
 def tb_checkpoint_unpack(codes, scales, dtype=torch.bfloat16):
     """The values that tb_checkpoint_pack's codes and scales stand for."""
+    xt, device = _PACKED_TYPES.get(dtype), _current_device()
+    if xt is None:
+        raise ValueError("activations are bfloat16 or float32")
     n_tok, d = codes.shape
     if tuple(scales.shape) != (n_tok, -(-d // 128)):
         raise ValueError("scales must be [n_tok][d / 128]")
-    x = torch.empty((n_tok, d), dtype=dtype, device=codes.device)
-    if _one_device((codes, scales)) != _current_device():
-        raise ValueError("tensors must live on the current device")
-    _check(load().tb_checkpoint_unpack(_ptr(codes, torch.int8), _ptr(scales, torch.float32), n_tok, d, _xtype(x), _ptr(x),
-                                       _stream()), "tb_checkpoint_unpack")
+    x = codes.new_empty((n_tok, d), dtype=dtype)
+    status = load().tb_checkpoint_unpack(_here(codes, device, torch.int8), _here(scales, device, torch.float32), n_tok, d, xt,
+                                         x.data_ptr(), _stream())
+    if status:
+        raise TurboBoAError(status, "tb_checkpoint_unpack")
     return x
 
 
