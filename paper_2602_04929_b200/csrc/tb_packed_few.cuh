@@ -210,7 +210,6 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int r0 = (blockIdx.x / cs) * RC, t0 = blockIdx.y * TB;
-  if (p.ad.n && threadIdx.x < TB) own[threadIdx.x] = t0 + (int)threadIdx.x < p.n_tok ? adapter_of(p.ad, t0 + threadIdx.x) : -1;
   // rows come eight at a time, d_out is a multiple of eight: those behind the last are taken to be the last eight and not stored
   const int eights = min(2 * MT, (p.w.d_out - r0) >> 3) - 1;
   const unsigned* row0 = p.w.packed + (long long)(r0 + g) * p.w.words;
@@ -219,6 +218,18 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
 #pragma unroll
   for (int n = 0; n < NT; ++n) x[n] = static_cast<const T*>(p.x) + (long long)min(t0 + 8 * n + g, p.n_tok - 1) * p.w.d_in;
   float sum[MT][NT][4] = {};
+  if (p.ad.n && warp == 7) {
+    // the tokens' adapters, and their rows towards this CTA's columns: the end of the kernel would wait for them
+    if (lane < TB) own[lane] = t0 + lane < p.n_tok ? adapter_of(p.ad, t0 + lane) : -1;
+    __syncwarp();
+    for (int e = lane; e < TB * p.ad.rank; e += 32) {
+      const int id = own[e / p.ad.rank];
+      if (id >= 0) {
+        const T* at = static_cast<const T*>(p.M) + ((long long)id * p.ad.rank + e % p.ad.rank) * p.w.d_out + r0;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+      }
+    }
+  }
   if constexpr (!NARROW) {
     constexpr int STAGE = RC * 128 * BITS;  // eight blocks of 16 BITS bytes a row: BITS pieces
     const int blocks = p.w.d_in >> 7, per_group = p.w.group >> 7;

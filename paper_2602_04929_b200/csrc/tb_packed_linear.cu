@@ -78,9 +78,11 @@ tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
 
 // Which product: few tokens in bf16, and float whatever their number, read the weights into registers; more go to tcgen05 tiles, whose
 // smallest has 32 tokens.  The gradient of float inputs runs on the FP32 pipe.
-enum { FEW_TOKENS = 16 };
+// Measured on 4096 x 4096, 4 bits / 8192 x 8192, 2 bits (us), registers / tiles: 24 tokens 13.9 / 17.1, 31.5 / 31.1; 32 tokens
+// 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.
+enum { FEW_TOKENS = 32 };
 static bool takes_few(tb_dtype type, long long n_tok, bool back) {
-  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= 65535ll * FEW_TOKENS);
+  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= 65535ll * 16);
 }
 
 // Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.

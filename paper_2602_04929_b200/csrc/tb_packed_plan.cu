@@ -20,6 +20,7 @@ struct PrepP {
 __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int b = blockIdx.x;
+  pdl_trigger();  // the product's CTAs may take their places
   if (b < p.sz_ctas) {
     __shared__ float s[32][33];
     __shared__ unsigned z[32][33];
@@ -44,6 +45,7 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
           reinterpret_cast<uint2*>(p.zt)[at] = make_uint2(z[lane][i], bf2(__floats2bfloat162_rn(v - hi, hi)));
         }
       }
+    pdl_wait();  // whoever waits for this kernel has waited for the one before it, beside which it may have run
     return;
   }
   b -= p.sz_ctas;
@@ -53,6 +55,7 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
       const int r = (int)(i / p.pitch), k = (int)(i - (long long)r * p.pitch);
       p.copy[i] = k < p.w.words ? p.w.packed[(long long)r * p.w.words + k] : 0u;
     }
+    pdl_wait();
     return;
   }
   b -= p.copy_ctas;
@@ -79,11 +82,13 @@ __global__ void __launch_bounds__(256) k_packed_prep(const PrepP p) {
     p.runs[t0 + at] = make_int4(t0 + tid, t0 + e, own[tid], 0);
   }
   if (tid == 0) p.n_runs[b] = all;
+  pdl_wait();
 }
 
 // out = the splits' sums, added in their order, and the adapters' share of the token, rounded once; four columns a thread.
 __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* out, long long n4, int cols4, int splits, const Adapt ad,
                                                      const float* low, const __nv_bfloat16* M) {
+  pdl_wait();
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n4; i += gridDim.x * 256ll) {
     float4 s = __ldcs(part + i);
     for (int k = 1; k < splits; ++k) {
@@ -99,7 +104,7 @@ __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* 
         float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 8
         for (int r = 0; r < ad.rank; ++r) {
-          const uint2 w = __ldg(m + (long long)r * cols4);
+          const uint2 w = m[(long long)r * cols4];
           const float v = l[r];
           a.x = fmaf(v, __uint_as_float(w.x << 16), a.x), a.y = fmaf(v, __uint_as_float(w.x & 0xffff0000u), a.y);
           a.z = fmaf(v, __uint_as_float(w.y << 16), a.z), a.w = fmaf(v, __uint_as_float(w.y & 0xffff0000u), a.w);
@@ -196,14 +201,18 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   q.sz_across = (w.n_g + 31) / 32;
   q.sz_ctas = q.sz_across * (p.rows_pad / 32);
   q.copy_ctas = q.copy ? (int)(((long long)w.d_out * p.pitch + 1023) / 1024) : 0;
-  k_packed_prep<<<(unsigned)(q.sz_ctas + q.copy_ctas + (p.n_runs ? t.t_tiles : 0)), 256, 0, st>>>(q);
+  const dim3 prep((unsigned)(q.sz_ctas + q.copy_ctas + (p.n_runs ? t.t_tiles : 0)));
+  if (ad.n)  // beside the kernel that makes x A^T, which started when all before it had ended
+    TB_CUDA_CHECK(launch_pdl(k_packed_prep, prep, dim3(256), 0, st, q));
+  else
+    k_packed_prep<<<prep, 256, 0, st>>>(q);
   TB_LAUNCH_CHECK();
   TB_TRY(back ? packed_tc_backward(p, xmap, wmap, t.pairs, st) : packed_tc_forward(p, xmap, wmap, t.pairs, st));
   if (t.splits > 1) {
     const long long n4 = (long long)p.n_tok * p.n_cols / 4;
     const long long nb = (n4 + 255) / 256;
-    k_packed_join<<<(unsigned)(nb < 4096 ? nb : 4096), 256, 0, st>>>(reinterpret_cast<const float4*>(p.part), reinterpret_cast<uint2*>(out), n4,
-                                                                          p.n_cols / 4, t.splits, ad, low, p.M);
+    TB_CUDA_CHECK(launch_pdl(k_packed_join, dim3((unsigned)(nb < 4096 ? nb : 4096)), dim3(256), 0, st, reinterpret_cast<const float4*>(p.part),
+                             reinterpret_cast<uint2*>(out), n4, p.n_cols / 4, t.splits, ad, low, p.M));
     TB_LAUNCH_CHECK();
   }
   return TB_OK;

@@ -192,6 +192,9 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
   cluster_barrier();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
+  // from here on, what the preparing kernel (and the one that makes x A^T) wrote is read; the operands were there before both
+  pdl_wait();
+  pdl_trigger();
   const int half_n = p.n_tile >> 1;
   const int n_tiles = p.m_tiles * p.t_tiles * p.splits;
   const int group = BACK ? p.n_sum : p.w.group;  // columns of a scale that leaves the sum
@@ -476,7 +479,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
 #pragma unroll
           for (int ch = 0; ch < 8; ++ch) {
             const int col = c.m0 + 64 * hf + 8 * ch;
-            v[ch] = m && col < p.n_cols ? __ldg(reinterpret_cast<const uint4*>(m + col)) : make_uint4(0u, 0u, 0u, 0u);
+            v[ch] = m && col < p.n_cols ? *reinterpret_cast<const uint4*>(m + col) : make_uint4(0u, 0u, 0u, 0u);
           }
           ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
           if (!ok) break;
@@ -588,7 +591,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             lora = true;
           }
           float s = 1.0f;
-          if (!lora) s = __ldg(p.st + (long long)parts.g * p.rows_pad + col);
+          if (!lora) s = p.st[(long long)parts.g * p.rows_pad + col];
           if (!acc_full()) break;
           const uint32_t taddr = tmem_row + (acc_it & 1u) * 256u;
 #pragma unroll
@@ -663,13 +666,15 @@ tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& xmap, const CUt
   cfg.blockDim = dim3(Roles<BACK>::THREADS);
   cfg.dynamicSmemBytes = PT_SMEM;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_packed_tc<BITS, BACK>, p, xmap, wmap));
   TB_LAUNCH_CHECK();
   return TB_OK;
