@@ -361,11 +361,12 @@ tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_
 // the rank its columns N, tokens the contraction, 64 of them a stage.  Both operands are written to shared memory by the producer
 // warps, as they are stored (M- and N-major, 128-byte swizzle): the input as it is, or its 8-bit codes as bf16 integers; low as
 // three bf16 pieces side by side (N = 3 RP), all 24 bits of it, times the codes' scale of its token and these 128 columns.  Tokens
-// behind the end of a request are zeros in both, so nothing of another request gets in.  The kernel is bound by reading the input
+// behind the end of a request are zeros in both, so nothing of another request gets in.  Full pieces of bf16 input come by TMA,
+// ahead of the producers.  The kernel is bound by reading the input
 // and, at high ranks, by making the pieces.  A CTA has one adapter's columns and, as one of a cluster, every cs-th piece of 64
 // tokens; accumulations end after 2048 tokens; the CTAs' sums are added in a fixed order through distributed shared memory.
 
-enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 32, AG_THREADS = 288 };  // AG_PART: stages of an accumulation
+enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 32, AG_THREADS = 320 };  // AG_PART: stages of an accumulation
 
 // RP: the rank, rounded up to 16, 32, 64 or 128.
 template <int RP>
@@ -400,7 +401,7 @@ __device__ __forceinline__ float rest_of(float v, unsigned bits) {  // of v with
 template <int RP, bool EIGHT>
 __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
     k_adapter_grad(Adapt ad, const void* __restrict__ in, const float* __restrict__ in_scales, const float* __restrict__ low, int n_tok,
-                   int width, float* __restrict__ G) {
+                   int width, float* __restrict__ G, const __grid_constant__ CUtensorMap imap) {
   using S = GradShape<RP>;
   extern __shared__ unsigned char ag_raw[];
   __shared__ __align__(8) unsigned long long bars[2 * S::STAGES + 1];
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int s = 0; s < S::STAGES; ++s) {
-      mbar_init(full_bar(s), 8);
+      mbar_init(full_bar(s), EIGHT ? 8 : 9);  // the producers', and that of the warp that fetches full pieces
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(done_bar, 1);
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
         const signed char* src = static_cast<const signed char*>(in) + (long long)(t + row) * width + c0 + 16 * u;
         xv[i] = row < n && c0 + 16 * u < width ? __ldcs(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
       }
-    } else {
+    } else if (n < AG_TOK) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = tid + 256 * i, row = e >> 4, u = e & 15;
@@ -467,7 +468,7 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
       lv[4 * k] = v.x, lv[4 * k + 1] = v.y, lv[4 * k + 2] = v.z, lv[4 * k + 3] = v.w;
     }
   };
-  auto store = [&](uint32_t stage) {
+  auto store = [&](uint32_t stage, int n) {
     if constexpr (EIGHT) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
         for (int h = 0; h < 2; ++h)
           sts16(at + ((((u & 3) * 2 + h) ^ (row & 7)) << 4), make_uint4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]));
       }
-    } else {
+    } else if (n < AG_TOK) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int e = tid + 256 * i, row = e >> 4, u = e & 15;
@@ -582,18 +583,32 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
     while (rq < n_piece && ok) {
       const uint32_t s = it % S::STAGES, ph = (it / S::STAGES) & 1u;
       const uint32_t stage = base + s * S::STAGE;
+      const int here = t, n_here = min(AG_TOK, piece[rq].y - t);
       advance((int)cs);
       const bool more = rq < n_piece, last = !more || in_part == AG_PART - 1;
       if (warp < 8) {
         ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(s), ph ^ 1u, &gave_up, &g_grad_error));
         if (ok) {
-          store(stage);
+          store(stage, n_here);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(full_bar(s));
           // (loads after the fence: it waits for all that its thread has in flight)
           if (more) fetch(t, min(AG_TOK, piece[rq].y - t));
           if (last) drain();
+        }
+      } else if (warp == 9) {
+        if (!EIGHT) {
+          ok = __all_sync(0xffffffffu, mbar_wait(empty_bar(s), ph ^ 1u, &gave_up, &g_grad_error));
+          if (ok && lane == 0) {
+            if (n_here == AG_TOK) {
+              mbar_expect_tx(full_bar(s), S::A_BYTES);
+              tma_load_2d(stage, &imap, c0, here, full_bar(s));
+              tma_load_2d(stage + 8192, &imap, c0 + 64, here, full_bar(s));
+            } else {
+              mbar_arrive(full_bar(s));
+            }
+          }
         }
       } else {
         ok = __all_sync(0xffffffffu, mbar_wait(full_bar(s), ph, &gave_up, &g_grad_error));
@@ -668,6 +683,10 @@ static tb_status launch_grad(const Adapt& ad, const void* in, const float* in_sc
   // CTAs along the tokens until an adapter that had nearly all of them would fill the GPU, while an even share is a stage at least
   int cs = 1;
   while (cs < 8 && cols * cs * 2 <= 2 * sms && n_tok / ad.n / (2 * cs) >= AG_TOK) cs *= 2;
+  CUtensorMap imap = {};
+  if (!EIGHT)
+    TB_TRY(make_map_2d(&imap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, in, (unsigned long long)width, (unsigned long long)n_tok, 64, AG_TOK,
+                       CU_TENSOR_MAP_SWIZZLE_128B));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(cols * cs), (unsigned)ad.n);
   cfg.blockDim = dim3(AG_THREADS);
@@ -680,7 +699,7 @@ static tb_status launch_grad(const Adapt& ad, const void* in, const float* in_sc
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_grad<RP, EIGHT>, ad, in, in_scales, low, n_tok, width, G));
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_grad<RP, EIGHT>, ad, in, in_scales, low, n_tok, width, G, imap));
   TB_LAUNCH_CHECK();
   return TB_OK;
 }

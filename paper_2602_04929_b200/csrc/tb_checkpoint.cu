@@ -4,30 +4,69 @@
 // 16-byte loads of float), so a run's maximum is four shuffles away and a warp stores 256 bytes of codes.  A lane has two
 // such pieces in flight.
 //
+// Packing is bound by its instructions as much as by HBM, about nine a value.  bf16 magnitudes are compared two at a time as
+// integers.  The scale's division is two fused steps on 1 / 127 (exact where nothing underflows).
+//
 // The codes are those of the true quotient.  y = x * (1 / scale) is off by less than 2^-14 where |y| <= 127, so rounding it decides
 // unless it lies that close to the middle between two codes.  Only a lane that has such a value looks further: the sign of x - (q +- 1/2) scale,
 // which one fused multiply-add gives exactly, says whether q is the nearest, and a tie (the sum is 0) goes to the even one.  Rounding
-// is one addition: 1.5 * 2^23 + y has the code in its low bits.
+// is one fused step: 1.5 * 2^23 + y has the code in its low bits.
 #include "tb_packed.cuh"
 
 namespace tb {
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-  const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
-  const unsigned w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// Eight neighbouring values as they are stored; the largest magnitude of half a warp's as the bits of a float, which order like the
+// values, with what is not finite on top.
+template <typename T>
+struct Words8;
+template <>
+struct Words8<__nv_bfloat16> {
+  unsigned w[4];
+  __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
+    w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
   }
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  __device__ __forceinline__ unsigned half_warp_top() const {
+    unsigned m = 0;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float4 q = __ldcs(reinterpret_cast<const float4*>(p) + h);
-    v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return max(m << 16, m & 0xffff0000u);
   }
-}
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+};
+template <>
+struct Words8<float> {
+  float f[8];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+  }
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 q = __ldcs(reinterpret_cast<const float4*>(p) + h);
+      f[4 * h] = q.x, f[4 * h + 1] = q.y, f[4 * h + 2] = q.z, f[4 * h + 3] = q.w;
+    }
+  }
+  __device__ __forceinline__ unsigned half_warp_top() const {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = f[i];
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   unsigned w[4];
 #pragma unroll
@@ -69,7 +108,7 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
                                                          unsigned long long per_inv) {
   const int half = threadIdx.x >> 4, l = threadIdx.x & 15;
   const long long r0 = (long long)blockIdx.x * (16 * CKPT_PER) + half;
-  float v[CKPT_PER][8];
+  Words8<T> raw[CKPT_PER];
   bool in[CKPT_PER];
   long long at[CKPT_PER];
 #pragma unroll
@@ -80,20 +119,25 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
     place_of(run, n_g, per_inv, l, t, col);
     in[k] = run < n_runs && col < d;
     at[k] = t * d + col;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
-    if (in[k]) load8(x + at[k], v[k]);
+    raw[k].zero();
+    if (in[k]) raw[k].load(x + at[k]);
   }
 #pragma unroll
   for (int k = 0; k < CKPT_PER; ++k) {
-    unsigned top = 0;  // magnitudes as integers: they order like the values, and what is not finite comes out on top
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const unsigned top = raw[k].half_warp_top();
     const bool finite = top < 0x7f800000u;
-    const float s = finite ? __fdiv_rn(__uint_as_float(top), 127.0f) : __uint_as_float(0x7fffffffu);
-    const float inv = __fdiv_rn(1.0f, s);
+    float s;
+    if (top >= 0x10000000u) {  // 2^-95 and more
+      constexpr float i127 = 1.0f / 127.0f;
+      const float t = __uint_as_float(top), q = t * i127;
+      s = finite ? fmaf(fmaf(-q, 127.0f, t), i127, q) : __uint_as_float(0x7fffffffu);
+    } else {
+      s = __fdiv_rn(__uint_as_float(top), 127.0f);
+    }
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    float v[8];
+    raw[k].values(v);
     unsigned w[2] = {0, 0};
     if (finite && s >= 1.17549435e-38f) {
       constexpr float magic = 12582912.0f;
@@ -101,13 +145,13 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
       float off = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = v[k][i] * inv, r = y + magic;
+        const float r = fmaf(v[i], inv, magic);
         q[i] = __float_as_uint(r);
-        off = fmaxf(off, fabsf(y - (r - magic)));
+        off = fmaxf(off, fabsf(fmaf(v[i], inv, magic - r)));
       }
       if (off > 0.5f - 6.1035156e-5f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = (unsigned)nearest_code(v[k][i], s, inv);
+        for (int i = 0; i < 8; ++i) q[i] = (unsigned)nearest_code(v[i], s, inv);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -117,7 +161,7 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
       constexpr float up = 18446744073709551616.0f;
       const float su = s * up, iu = 1.0f / su;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i >> 2] |= ((unsigned)nearest_code(v[k][i] * up, su, iu) & 0xffu) << (8 * (i & 3));
+      for (int i = 0; i < 8; ++i) w[i >> 2] |= ((unsigned)nearest_code(v[i] * up, su, iu) & 0xffu) << (8 * (i & 3));
     }
     if (in[k]) *reinterpret_cast<uint2*>(codes + at[k]) = make_uint2(w[0], w[1]);
     if (l == 0 && r0 + 16 * k < n_runs) scales[r0 + 16 * k] = s;
