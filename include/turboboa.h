@@ -315,9 +315,10 @@ typedef struct {
                                  divides d_in                                       */
   const unsigned int* packed; /* [d_out][d_in * bits / 32], 16-byte aligned         */
   const float* scales;        /* [d_out][n_g]                                       */
-  const int* zeros;           /* [d_out][n_g]; -128 .. 255 on the tensor-core paths
-                                 (the quantizer's lie in 0 .. 2^bits - 1): beyond,
-                                 code - zero is rounded to bf16's eight bits        */
+  const int* zeros;           /* [d_out][n_g].  The quantizer's, 0 .. 2^bits - 1, and
+                                 any in -128 .. 128 are exact; where code - zero
+                                 needs more than bf16's eight bits, it is rounded
+                                 to about as many (not in dx of float activations) */
 } tb_packed_weight;
 
 /* Low-rank adapters of the requests in a batch.  Request j has the tokens starts[j] ..

@@ -142,10 +142,10 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
 // The same for many tokens, on tcgen05: 128 tokens are the rows M of the tile, the rank its columns N, both operands by TMA as they
 // are stored (K-major).  x so is read once, at HBM's rate, and an adapter once for 128 tokens.  A tile's adapters (AL_COLS / N of
 // them, more in further CTAs) are gone through one after the other, each into columns of its own; rows of other adapters are computed and dropped.
-// CTAs of a cluster share the contraction; an accumulation ends after 2048 columns where tensor memory has room for more of them.
+// CTAs of a cluster share the contraction; an accumulation ends after 512 columns where tensor memory has room for more of them (every step may drop the last bit).
 
 enum { LOW_TC_WORK = 65536 };  // tokens x rank
-enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_PART = 2048, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
+enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_PART = 512, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
 
 struct LowTc {
   Adapt ad;
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
     for (int a = 0; a < ids && ok; ++a) {
       int in_part = 0, part = 0;
       for (int st = 0; st < n_st; ++st) {
-        ok = mbar_wait(full_bar(s), phase, &gave_up, &g_grad_error);
+        ok = __all_sync(0xffffffffu, mbar_wait(full_bar(s), phase, &gave_up, &g_grad_error));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (one) {
@@ -249,6 +249,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
           for (int kk = 0; kk < 4; ++kk) umma_bf16(d, x + 2 * kk, m + 2 * kk, idesc, in_part > 0 || kk > 0 ? 1u : 0u);
           umma_commit(empty_bar(s));
         }
+        __syncwarp();
         if (++in_part == p.part) in_part = 0, ++part;
         if (++s == p.stages) s = 0, phase ^= 1u;
       }
@@ -292,6 +293,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
     else
       __syncthreads();
   }
+  settle(*(volatile int*)&gave_up);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)AL_COLS) : "memory");
@@ -632,6 +634,8 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
     }
     __syncthreads();
   }
+  settle(*(volatile int*)&gave_up);
+  __syncthreads();
   // (every MMA has been drained: the sums may take the stages' place)
   if (warp < 8) {
     const int c = (warp & 3) * 32 + lane;

@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
       }
       if (++s == p.stages) s = 0, phase ^= 1u;
     }
+    settle(*(volatile int*)&gave_up);
     __syncthreads();  // the ring becomes the sums'
   } else {
     const int runs = p.w.d_in >> 5, per_group = p.w.group >> 5;

@@ -91,9 +91,13 @@ struct Raw {
     PAD = (BYTES + 1023) & ~1023,  // swizzled rows start on a multiple of their pattern
     MMA_STAGES = BITS <= 4 ? 6 : 4,  // even: the MMA warp takes two at a time
     ROOM = PT_SMEM - 1024 - 512 - MMA_STAGES * PT_STAGE_BYTES,
-    STAGES = ROOM / PAD < 8 ? ROOM / PAD : 8
+    TURNS = BACK ? 4 : 2,  // decode warpgroups, which take the units in turn
+    FIT = ROOM / PAD < 8 ? ROOM / PAD : 8,
+    // a whole number of turns, so that a slot is always the same warpgroup's: waits go by parity, and one that skipped a phase of
+    // the barrier that it looks at would take the phase before for its own
+    STAGES = FIT / TURNS * TURNS
   };
-  static_assert(STAGES >= 2, "the ring holds two units at least");
+  static_assert(STAGES >= TURNS, "the ring holds a unit for every warpgroup");
   // 16-byte piece c of row r
   static __device__ __forceinline__ uint32_t piece(int r, int c) {
     if constexpr (ROW == 32) return r * ROW + ((c ^ ((r >> 2) & 1)) << 4);
@@ -135,7 +139,7 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
 
 template <bool BACK>
 struct Roles {
-  enum { DECODE = BACK ? 4 : 2, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
+  enum { DECODE = Raw<2, BACK>::TURNS, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
 };
 
 template <int BITS, bool BACK>
@@ -149,17 +153,20 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
   unsigned char* gen_base = pt_smem_raw + (base - raw);
   const uint32_t raw_base = base + STAGES * PT_STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(gen_base + (PT_SMEM - 1024 - 512));
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4 + 16);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4 + 17);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* odd_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);  // adapters hold what is not finite (once seen, stays)
   const uint32_t bar0 = smem_u32(bars);
-  // full: in CTA 0, its TMA warp and the decode warps of both CTAs (four a stage each) arrive, and the bytes of both; empty, accf: in
-  // both, from the commits of CTA 0; acce: in CTA 0, the epilogue warps of both
+  // full: in CTA 0, the TMA warps and the decode warps of both CTAs (four a stage each) arrive, and the bytes of both; empty, accf: in
+  // both, from the commits of CTA 0; acce: in CTA 0, the epilogue warps of both; tile: the decode warps, between tiles with adapters.
+  // Waits go by parity, so a barrier must never be two phases from what a wait takes it for: whoever waits for a stage also fills it,
+  // and has filled one at most STAGES before, or knows that all those of the tile before are filled.
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
   auto accf_bar = [&](int b) { return bar0 + 8u * (2 * STAGES + b); };
   auto acce_bar = [&](int b) { return bar0 + 8u * (2 * STAGES + 2 + b); };
   auto raw_full = [&](int s) { return bar0 + 8u * (2 * STAGES + 4 + s); };   // a unit's bytes are in the ring
+  const uint32_t tile_bar = bar0 + 8u * (2 * STAGES + 20);
   auto raw_empty = [&](int s) { return bar0 + 8u * (2 * STAGES + 12 + s); };  // the decode warps that it belongs to have read it
 
   uint32_t rank;
@@ -168,7 +175,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(full_bar(s), 1 + 8);
+      mbar_init(full_bar(s), 2 + 8);
       mbar_init(empty_bar(s), 1);
     }
     for (int s = 0; s < 8; ++s) {
@@ -179,6 +186,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       mbar_init(accf_bar(b), 1);
       mbar_init(acce_bar(b), 2 * R::EPILOGUE);
     }
+    mbar_init(tile_bar, 4 * R::DECODE);
     *abort_flag = 0;
     *odd_flag = 0;
     mbar_fence_init();
@@ -232,11 +240,14 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             break;
           }
           if (st < n_st) {
-            if (rank == 0) mbar_expect_tx(full_bar(s), 2u * half_n * PT_BK * 2u);
+            if (rank == 0)
+              mbar_expect_tx(full_bar(s), 2u * half_n * PT_BK * 2u);
+            else
+              mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
             tma_load_2d_pair(base + s * PT_STAGE_BYTES + PT_A_BYTES, &xmap, c.k0 + st * PT_BK, c.t0 + (int)rank * half_n,
                              map_to_rank(full_bar(s), 0));
-          } else if (rank == 0) {
-            mbar_arrive(full_bar(s));
+          } else {
+            mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
           }
         }
       }
@@ -252,7 +263,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       const uint64_t b_main = smem_desc_k_sw128(base + PT_A_BYTES);
       constexpr uint32_t a_step = (BACK ? 2048 : 32) >> 4, l_step = 2048 >> 4, b_step = 32 >> 4;
       Parts parts(group);
-      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, &g_packed_error); };
+      auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_flag, &g_packed_error); };
       auto acc_free = [&]() {
         const bool got = wait(acce_bar(acc_it & 1u), ((acc_it >> 1) & 1u) ^ 1u);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -288,6 +299,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               four(d, a_main + at, b_main + at, more);
               umma_commit_pair(empty_bar(s));
             }
+            __syncwarp();
             ok = wait(full_bar(s + 1), phase);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (!ok) break;
@@ -297,6 +309,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               umma_commit_pair(empty_bar(s + 1));
               if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
             }
+            __syncwarp();
             more = 1;
             if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
             s += 2;
@@ -329,11 +342,13 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
                 umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, ad + kk * a_step, bd + kk * b_step, id_main, more);
                 if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
               }
+              __syncwarp();
               k += 16;
               if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
             }
             if (!ok) break;
             if (one) umma_commit_pair(empty_bar(s));
+            __syncwarp();
           } else {
             if (!BACK && st == n_st) {  // forward, an accumulation of their own: no scale applies to them
               ok = acc_free();
@@ -348,6 +363,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               umma_commit_pair(empty_bar(s));
               if (last) umma_commit_pair(accf_bar(acc_it & 1u));
             }
+            __syncwarp();
             if (last) ++acc_it;
           }
           if (++s == STAGES) s = 0, phase ^= 1u;
@@ -402,11 +418,16 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     const uint32_t sw = (uint32_t)(my_row & 7);
     const bool one_sz = p.w.group % 128 == 0;
     constexpr int PER = BACK ? 1 : 2;  // stages of a unit
-    uint32_t it = 0, unit = 0;
+    uint32_t it = 0, unit = 0, tiles = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile c = tile_of(t);
       const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
+      if (p.n_runs && tiles > 0) {
+        ok = mbar_wait_warp(tile_bar, (tiles - 1) & 1u, abort_flag, &g_packed_error);
+        if (!ok) break;
+      }
+      ++tiles;
       for (int st = 0; st < n_st && ok; st += PER, ++unit) {
         const int here = min(PER, n_st - st);
         if ((int)(unit % R::DECODE) != turn) {
@@ -465,7 +486,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       // the adapters (where the sum is not split): four slots a stage, slot = (run, 16 of the rank, piece)
       const int n_slots = c.n_runs * nb * 2;
       for (int st = 0; st < c.lora && ok; ++st, ++it) {
-        if ((int)(it % R::DECODE) != turn) continue;
+        if ((int)((unit + st / PER) % R::DECODE) != turn) continue;  // as if they were further units
         const int s = it % STAGES;
         const uint32_t sa = base + s * PT_STAGE_BYTES, sb = sa + PT_A_BYTES;
         {
@@ -530,6 +551,10 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
+      }
+      if (p.n_runs) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tile_bar);
       }
     }
   } else {
@@ -638,6 +663,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     }
   }
 
+  settle(*abort_flag);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   cluster_barrier();

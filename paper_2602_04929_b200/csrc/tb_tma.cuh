@@ -52,6 +52,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
   return true;
 }
+// At the end of a kernel whose waits may have given up: copies and products still under way then get about 0.2 ms to end in.
+__device__ __forceinline__ void settle(bool gave_up) {
+  if (gave_up)
+    for (const long long t0 = clock64(); clock64() - t0 < 400000;) {
+    }
+}
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),

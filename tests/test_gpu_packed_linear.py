@@ -317,3 +317,176 @@ def test_8_bit_form_of_what_is_not_finite():
     assert torch.equal(torch.isnan(scales).cpu(), bad)
     assert torch.equal(torch.isnan(v), bad.repeat_interleave(128, 1)[:, :288])
     assert ((v[3] - 1).abs() < 1e-6).all()
+
+
+@pytest.mark.parametrize("n_tok,rows,d,rank,n_req,seed", [(24, 136, 640, 16, 24, 0), (32, 1032, 1024, 24, 9, 1), (40, 264, 2048, 16, 40, 2),
+                                                          (64, 520, 4096, 8, 64, 3), (100, 264, 3584, 64, 7, 4), (257, 1544, 1024, 16, 60, 5),
+                                                          (700, 264, 384, 8, 600, 6), (640, 2056, 256, 40, 5, 7)])
+def test_many_requests(n_tok, rows, d, rank, n_req, seed):
+    """Requests of every length at the sizes where tiles, splits of the contraction and the adapters' ways change."""
+    tb = _tb()
+    r = torch.Generator().manual_seed(seed)
+    cuts = torch.sort(torch.randint(0, n_tok + 1, (n_req - 1,), generator=r))[0].tolist()
+    starts = list(range(n_tok + 1)) if n_req == n_tok else [0] + cuts + [n_tok]
+    ids = torch.randint(-1, 12, (n_req,), generator=r).tolist()
+    p = pu.problem(seed, n_tok, rows, d, 2 + seed % 4, 128, BF, 11, rank, starts, ids)
+    _forward(p)
+    w, a = pu.on_gpu(tb, p)
+    xa = pu.forward64(p)[1].float()
+    want = pu.backward64(p, None, xa)
+    for got, name in zip(tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, x=p["x"].cuda(), xa=xa.cuda()), ("dx", "dA", "dB")):
+        pu.near(got, *want[name], name)
+    assert tb.tb_device_error_flag() == 0
+
+
+def test_more_adapters_in_a_tile_than_fit_side_by_side():
+    starts = [0, 10, 20, 30, 40, 50, 60, 70, 80, 600]
+    _forward(pu.problem(8, 600, 136, 4096, 4, 128, BF, 9, 128, starts, [3, 1, 4, 8, 5, 0, 2, 6, 7]))
+
+
+@pytest.mark.parametrize("rank", [8, 128])
+def test_long_contractions_of_the_narrow_product(rank):
+    """A CTA with 8192 columns ends its accumulations on the way; the reference in double on the GPU."""
+    tb = _tb()
+    n_tok, d = 10100, 8192
+    p = pu.problem(5, 1, 8, d, 2, 0, BF, 2, rank, [0, 1], [0])
+    w, _ = pu.on_gpu(tb, p)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((n_tok, d), generator=g, device="cuda").to(BF)
+    starts, ids = torch.tensor([0, 4000, n_tok], dtype=torch.int32).cuda(), torch.tensor([1, 0], dtype=torch.int32).cuda()
+    A, B = p["A"].cuda(), p["B"].cuda()
+    y, xa = tb.tb_packed_linear(w, x, tb.adapters(A, B, p["scale"].cuda(), starts, ids))
+    want = torch.cat([x[:4000].double() @ A[1].double().T, x[4000:].double() @ A[0].double().T])
+    # a step of 16 columns may drop up to 2^-23 of the running sum, which averages 2/3 of the final one (it grows like a root); an
+    # accumulation has 32 steps, or with ranks above 32 as many as a quarter of the 8192 columns has: 128
+    assert ((xa - want).norm() / want.norm()).item() <= 2 / 3 * (32 if rank == 8 else 128) * 2.0 ** -23
+    assert (xa - want).abs().max().item() <= (d + 64) * 2.0 ** -23 * (x.double().abs() @ A.double().abs().amax(0).T).max().item()
+    assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("rank", [16, 64, 128])
+@pytest.mark.parametrize("kept", ["full", "8 bits"])
+def test_gradients_of_many_tokens(rank, kept):
+    """A CTA with more than 2048 tokens ends its accumulations on the way; the reference in double on the GPU."""
+    tb = _tb()
+    n_tok, d, rows = 21003, 128, 136
+    p = pu.problem(6, 1, rows, d, 4, 0, BF, 2, rank, [0, 1], [0])
+    w, _ = pu.on_gpu(tb, p)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, dy = (torch.randn((n_tok, n), generator=g, device="cuda").to(BF) for n in (d, rows))
+    xa = torch.randn((n_tok, rank), generator=g, device="cuda")
+    starts, ids = torch.tensor([0, 20000, n_tok], dtype=torch.int32).cuda(), torch.tensor([1, 0], dtype=torch.int32).cuda()
+    A, B, c = p["A"].cuda(), p["B"].cuda(), p["scale"].cuda()
+    codes = tb.tb_checkpoint_pack(x)
+    how = dict(x=x) if kept == "full" else dict(checkpoint=codes)
+    xin = x.double() if kept == "full" else codes[0].double() * codes[1].double()
+    _, dA, dB = tb.tb_packed_linear_backward(w, dy, tb.adapters(A, B, c, starts, ids), xa=xa, want_dx=False, **how)
+    for i, tok in ((1, slice(0, 20000)), (0, slice(20000, n_tok))):
+        u = c[i].double() * (dy[tok].double() @ B[i].double().T)
+        for got, want in ((dA[i], u.T @ xin[tok]), (dB[i], c[i].double() * (xa[tok].double().T @ dy[tok].double()))):
+            assert ((got - want).norm() / want.norm()).item() <= 3e-6
+    assert tb.tb_device_error_flag() == 0
+
+
+def test_offsets_beyond_32_bits():
+    """270 000 tokens of 8192 columns: 2.2e9 values.  The first, a middle and the last tokens against a call on them alone."""
+    tb = _tb()
+    n_tok, d, rows = 270000, 8192, 8
+    p = pu.problem(7, 1, rows, d, 2, 128, BF, 1, 8, [0, 1], [0])
+    w, _ = pu.on_gpu(tb, p)
+    x = torch.empty((n_tok, d), dtype=BF, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for t in range(0, n_tok, 30000):
+        x[t:t + 30000].normal_(generator=g)
+    dy = torch.randn((n_tok, rows), generator=g, device="cuda").to(BF)
+    def batch(n):
+        return tb.adapters(p["A"].cuda(), p["B"].cuda(), p["scale"].cuda(), torch.tensor([0, n], dtype=torch.int32).cuda(),
+                           torch.tensor([0], dtype=torch.int32).cuda())
+    y, xa = tb.tb_packed_linear(w, x, batch(n_tok))
+    dx, _, _ = tb.tb_packed_linear_backward(w, dy, batch(n_tok))
+    codes, scales = tb.tb_checkpoint_pack(x)
+    for t in (0, 131072, n_tok - 64):
+        s = slice(t, t + 64)
+        y1, xa1 = tb.tb_packed_linear(w, x[s].clone(), batch(64))
+        assert (y[s].float() - y1.float()).norm() <= 0.01 * y1.float().norm() and (xa[s] - xa1).norm() <= 1e-5 * xa1.norm()
+        dx1, _, _ = tb.tb_packed_linear_backward(w, dy[s].clone(), batch(64))
+        assert (dx[s].float() - dx1.float()).norm() <= 0.01 * dx1.float().norm()
+        c1, s1 = tb.tb_checkpoint_pack(x[s].clone())
+        assert torch.equal(codes[s], c1) and torch.equal(scales[s], s1)
+    assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("bits,n_tok", [(2, 5), (3, 70), (4, 70), (7, 5), (7, 70), (8, 5), (8, 70)])
+def test_zero_points_outside_the_codes(bits, n_tok):
+    p = pu.problem(bits, n_tok, 136, 256, bits, 128, BF)
+    z = torch.randint(-128, 129, p["zeros"].shape, generator=torch.Generator().manual_seed(bits), dtype=torch.int32)
+    zd = (p["zeros"] - z).double().repeat_interleave(128, 1) * p["scales"].double().repeat_interleave(128, 1)
+    p["zeros"], p["Q"] = z, p["Q"] + zd
+    if bits < 8:
+        _forward(p)
+        return
+    # codes up to 255: c - z goes beyond 256 and is rounded to bf16, by 2^-8 of it at most, which is 2^-8 of the product's magnitudes
+    tb = _tb()
+    w, _ = pu.on_gpu(tb, p)
+    want, _, bound = pu.forward64(p)
+    pu.near(tb.tb_packed_linear(w, p["x"].cuda())[0], want, bound + 1.01 * 2.0 ** -8 * (p["x"].double().abs() @ p["Q"].abs().T))
+
+
+def test_refusals():
+    tb = _tb()
+    p = pu.problem(1, 40, 64, 128, 4, 0, BF, 2, 8, [0, 40], [0])
+    w, a = pu.on_gpu(tb, p)
+    x, dy = p["x"].cuda(), p["dy"].cuda()
+    xa = torch.zeros((40, 8), device="cuda")
+    bad = [lambda: tb.tb_packed_linear(w, p["x"], a), lambda: tb.tb_packed_linear(w, x.half(), a), lambda: tb.tb_packed_linear(w, x.float(), a),
+           lambda: tb.tb_packed_linear(w, x[:, :96].contiguous()), lambda: tb.tb_packed_linear(w, x.T.contiguous().T),
+           lambda: tb.tb_packed_linear(w, x, y=dy[:3]), lambda: tb.tb_packed_linear(w, x, a, xa=xa[:, :4]),
+           lambda: tb.tb_packed_linear(w, x, y=dy.float()), lambda: tb.tb_packed_linear_backward(w, x),
+           lambda: tb.tb_packed_linear_backward(w, dy, a, x=x), lambda: tb.tb_packed_linear_backward(w, dy, a, x=x[:20], xa=xa),
+           lambda: tb.tb_packed_linear_backward(w, dy, a, x=x.float(), xa=xa), lambda: tb.tb_checkpoint_pack(p["x"]),
+           lambda: tb.tb_checkpoint_pack(x.half()), lambda: tb.tb_checkpoint_unpack(x.to(torch.int8), xa),
+           lambda: tb.tb_packed_linear(w, x, ws=torch.empty(1 << 20, dtype=torch.uint8))]
+    for k, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {k} was taken")
+    both = tb.tb_checkpoint_pack(x)
+    for call, status in ((lambda: tb.tb_packed_linear(w, x, a, ws=torch.empty(256, dtype=torch.uint8, device="cuda")), 3),
+                         (lambda: tb.tb_packed_linear_backward(w, dy, a, x=x, checkpoint=both, xa=xa), 1),
+                         (lambda: tb.tb_packed_linear_backward(w, dy, want_dx=False), 1)):
+        with pytest.raises(tb.TurboBoAError) as e:
+            call()
+        assert e.value.status == status
+    need = tb.load().tb_packed_linear_workspace(w.address, a.address, 1, 40)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    y, _ = tb.tb_packed_linear(w, x, a, ws=ws)
+    assert torch.equal(y, tb.tb_packed_linear(w, x, a)[0])
+
+
+@pytest.mark.parametrize("n_tok,rows,d,bits,group", [(20000, 40, 520 - 8, 2, 0), (9000, 264, 96, 3, 96), (33000, 8, 160, 7, 32), (5000, 1032, 1056, 4, 0)])
+def test_many_tiles_for_every_pair_of_processors(n_tok, rows, d, bits, group):
+    """Short contractions and many tiles, with adapters' stages between them; the reference in double on the GPU."""
+    tb = _tb()
+    rank = 24
+    p = pu.problem(11, 1, rows, d, bits, group, BF, 3, rank, [0, 1], [0])
+    w, _ = pu.on_gpu(tb, p)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x, dy = (torch.randn((n_tok, n), generator=g, device="cuda").to(BF) for n in (d, rows))
+    cuts = torch.sort(torch.randint(0, n_tok, (149,), generator=g, device="cuda"))[0].tolist()
+    ids = torch.randint(-1, 3, (150,), generator=g, device="cuda")
+    at = [0] + cuts + [n_tok]
+    a = tb.adapters(p["A"].cuda(), p["B"].cuda(), p["scale"].cuda(), torch.tensor(at, dtype=torch.int32).cuda(), ids.to(torch.int32))
+    Q, A, B, c = p["Q"].cuda(), p["A"].cuda().double(), p["B"].cuda().double(), p["scale"].cuda().double()
+    y64, dx64 = x.double() @ Q.T, dy.double() @ Q
+    for j, i in enumerate(ids.tolist()):
+        if i >= 0:
+            s = slice(at[j], at[j + 1])
+            y64[s] += c[i] * ((x[s].double() @ A[i].T) @ B[i])
+            dx64[s] += c[i] * ((dy[s].double() @ B[i].T) @ A[i])
+    for _ in range(3):
+        y, xa = tb.tb_packed_linear(w, x, a)
+        dx, dA, dB = tb.tb_packed_linear_backward(w, dy, a, x=x, xa=xa)
+        assert tb.tb_device_error_flag() == 0
+        # every token by itself: a rounding of its values, backward one of the weights too
+        assert ((y - y64).norm(dim=1) <= 1.01 * 2.0 ** -8 * y64.norm(dim=1) + 1e-30).all()
+        assert ((dx - dx64).norm(dim=1) <= 2.02 * 2.0 ** -8 * dx64.norm(dim=1) + 2.0 ** -8 * dy.double().norm(dim=1) * Q.norm(dim=1).max()).all()
