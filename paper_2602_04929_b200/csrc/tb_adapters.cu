@@ -366,9 +366,9 @@ tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_
 // behind the end of a request are zeros in both, so nothing of another request gets in.  Full pieces of bf16 input come by TMA,
 // ahead of the producers.  The kernel is bound by reading the input
 // and, at high ranks, by making the pieces.  A CTA has one adapter's columns and, as one of a cluster, every cs-th piece of 64
-// tokens; accumulations end after 2048 tokens; the CTAs' sums are added in a fixed order through distributed shared memory.
+// tokens; accumulations end after 256 tokens (every step of 16 may drop the last bit); the CTAs' sums are added in a fixed order through distributed shared memory.
 
-enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 32, AG_THREADS = 320 };  // AG_PART: stages of an accumulation
+enum { AG_TOK = 64, AG_COLS = 128, AG_PART = 4, AG_THREADS = 320 };  // AG_PART: stages of an accumulation
 
 // RP: the rank, rounded up to 16, 32, 64 or 128.
 template <int RP>
