@@ -4,11 +4,10 @@
 // 16-byte loads of float), so a run's maximum is four shuffles away and a warp stores 256 bytes of codes.  A lane has two
 // such pieces in flight.
 //
-// Packing is bound by its instructions as much as by HBM, about nine a value.  bf16 magnitudes are compared two at a time as
-// integers.  The scale's division is two fused steps on 1 / 127 (exact where nothing underflows).
+// Packing is bound by its instructions as much as by HBM, about nine a value.  bf16 magnitudes are compared two at a time.  The scale's division is two fused steps on 1 / 127 (exact where nothing underflows).
 //
 // The codes are those of the true quotient.  y = x * (1 / scale) is off by less than 2^-14 where |y| <= 127, so rounding it decides
-// unless it lies that close to the middle between two codes.  Only a lane that has such a value looks further: the sign of x - (q +- 1/2) scale,
+// unless it lies that close to the middle between two codes.  Only such a value is looked at further: the sign of x - (q +- 1/2) scale,
 // which one fused multiply-add gives exactly, says whether q is the nearest, and a tie (the sum is 0) goes to the even one.  Rounding
 // is one fused step: 1.5 * 2^23 + y has the code in its low bits.
 #include "tb_packed.cuh"
@@ -22,18 +21,22 @@ struct Words8;
 template <>
 struct Words8<__nv_bfloat16> {
   unsigned w[4];
+  static __device__ __forceinline__ unsigned max2(unsigned a, unsigned b) {  // what is no number wins
+    unsigned o;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+  }
   __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
   __device__ __forceinline__ void load(const __nv_bfloat16* p) {
     const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
     w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
   }
   __device__ __forceinline__ unsigned half_warp_top() const {
-    unsigned m = 0;
+    unsigned m = max2(max2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), max2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+    m = max2(m, __byte_perm(m, 0, 0x1032));  // both halves, so that one shuffle carries the same twice
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-    return max(m << 16, m & 0xffff0000u);
+    for (int o = 1; o < 16; o <<= 1) m = max2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m & 0xffff0000u;
   }
   __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
@@ -139,25 +142,25 @@ __global__ void __launch_bounds__(256) k_checkpoint_pack(const T* __restrict__ x
     float v[8];
     raw[k].values(v);
     unsigned w[2] = {0, 0};
-    if (finite && s >= 1.17549435e-38f) {
+    if (finite && s >= 7.9e-31f) {  // 2^-100: no product below underflows
       constexpr float magic = 12582912.0f;
       unsigned q[8];
-      float off = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float r = fmaf(v[i], inv, magic);
         q[i] = __float_as_uint(r);
-        off = fmaxf(off, fabsf(fmaf(v[i], inv, magic - r)));
-      }
-      if (off > 0.5f - 6.1035156e-5f) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = (unsigned)nearest_code(v[i], s, inv);
+        // value by value: half of a bf16 run's maximum is a tie, so that nearly every second warp has one among its 256
+        const float near = r - magic, d = fmaf(v[i], inv, -near);
+        if (fabsf(d) > 0.5f - 6.1035156e-5f) {  // near or its neighbour on d's side: whose side of the middle is x on?
+          const float half = copysignf(0.5f, d), e = fmaf(-(near + half), s, v[i]) * half;
+          if (e > 0.0f || (e == 0.0f && (q[i] & 1u))) q[i] += half > 0.0f ? 1u : 0xffffffffu;
+        }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         w[h] = __byte_perm(__byte_perm(q[4 * h], q[4 * h + 1], 0x0040), __byte_perm(q[4 * h + 2], q[4 * h + 3], 0x0040), 0x5410);
     } else if (finite && s > 0.0f) {
-      // a scale below 2^-126 has no float reciprocal worth the name: scaled up by 2^64 it has, and so has x
+      // a smaller scale is scaled up by 2^64 first, and so is x
       constexpr float up = 18446744073709551616.0f;
       const float su = s * up, iu = 1.0f / su;
 #pragma unroll
