@@ -27,8 +27,8 @@ static __device__ int g_grad_error = 0;
 // sums are added in a fixed order.
 
 template <int NT>
-__global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat16* __restrict__ in, const __nv_bfloat16* __restrict__ M,
-                                                     int n_tok, int width, float* __restrict__ low) {
+__global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width,
+                                                     float* low, int late) {
   constexpr int TT = 16, KG = 8, R = 8 * NT, PITCH = R + 1;
   __shared__ int own[TT], pick;
   __shared__ float sum[TT * PITCH];
@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
       if (own[t] == -1 && r < ad.rank) low[(long long)(t0 + t) * ad.rank + r] = 0.0f;
     }
   const int id = pick;
+  if (id < 0 && late) pdl_wait();  // `late`: launched beside a product; whoever waits for this kernel waits for both
   if (id < 0) return;  // the same in every CTA of the cluster
   const int g = lane >> 2, q = lane & 3;
   const __nv_bfloat16* xr[2];
@@ -75,9 +76,9 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
     const bool in_k = k < width;
     uint4 x[2], m[NT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = in_k && xr[i] ? __ldg(reinterpret_cast<const uint4*>(xr[i] + k)) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < 2; ++i) x[i] = in_k && xr[i] ? *reinterpret_cast<const uint4*>(xr[i] + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) m[n] = in_k && mr[n] ? __ldg(reinterpret_cast<const uint4*>(mr[n] + k)) : make_uint4(0, 0, 0, 0);
+    for (int n = 0; n < NT; ++n) m[n] = in_k && mr[n] ? *reinterpret_cast<const uint4*>(mr[n] + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       mma_bf16(acc[n], x[0].x, x[1].x, x[0].y, x[1].y, m[n].x, m[n].y);
@@ -110,11 +111,12 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
     low[(long long)(t0 + t) * ad.rank + r0 + r] = v;
   }
   if (cs > 1) cluster_barrier();  // nobody leaves while its sums are read
+  if (late) pdl_wait();
 }
 
 template <int NT>
 static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
-                            cudaStream_t st) {
+                            cudaStream_t st, bool late) {
   constexpr int TT = 16;
   const int tiles = (n_tok + TT - 1) / TT, zs = (ad.rank + 63) / 64;
   const int ys = min(TT, min(ad.n_req, ad.n));
@@ -127,14 +129,16 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
   cfg.gridDim = dim3((unsigned)(tiles * cs), (unsigned)ys, (unsigned)zs);
   cfg.blockDim = dim3(256);
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)cs;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low<NT>, ad, in, M, n_tok, width, low));
+  cfg.numAttrs = late ? 2 : 1;
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low<NT>, ad, in, M, n_tok, width, low, (int)late));
   TB_LAUNCH_CHECK();
   return TB_OK;
 }
@@ -177,6 +181,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
     gave_up = 0;
     mbar_fence_init();
   }
+  if (tid == 160) prefetch_map(&xmap), prefetch_map(&mmap);
   if (tid < AL_TOK) own[tid] = t0 + tid < p.n_tok ? adapter_of(p.ad, t0 + tid) : -2;
   __syncthreads();
   {
@@ -342,17 +347,22 @@ static tb_status launch_low_tc(const Adapt& ad, const __nv_bfloat16* in, const _
   return TB_OK;
 }
 
-// low [n_tok][rank] = in M_i^T for the adapter i of every token, zero for a token without one.
-tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
+// Tiles of 16 tokens start sooner and compute less for rows of other adapters, but read an adapter once for every 16 tokens.
+// Measured, tiles of 16 / tcgen05: 512 x 4096, rank 16, 6.4 / 8.6 us; 1999 x 4096, rank 32, 23 requests, 13.9 / 17.6 us;
+// 1024 x 8192, rank 64, 29 / 20 us; 4099 x 8192, rank 64, 68 (tiles of 64) / 36 us.
+bool adapter_low_in_small_tiles(const Adapt& ad, int n_tok) {
+  return (long long)n_tok * ad.rank < LOW_TC_WORK || (long long)n_tok / ad.n_req < 48;
+}
+
+// low [n_tok][rank] = in M_i^T for the adapter i of every token, zero for a token without one.  `late` (small tiles only): the call
+// before on the stream is a product that does not need it, and the one after waits for both.
+tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, bool late,
                            cudaStream_t st) {
-  // Tiles of 16 tokens start sooner and compute less for rows of other adapters, but read an adapter once for every 16 tokens.
-  // Measured, tiles of 16 / tcgen05: 512 x 4096, rank 16, 6.4 / 8.6 us; 1999 x 4096, rank 32, 23 requests, 13.9 / 17.6 us;
-  // 1024 x 8192, rank 64, 29 / 20 us; 4099 x 8192, rank 64, 68 (tiles of 64) / 36 us.
-  if ((long long)n_tok * ad.rank < LOW_TC_WORK || (long long)n_tok / ad.n_req < 48) {
-    if (ad.rank <= 8) return launch_low<1>(ad, in, M, n_tok, width, low, st);
-    if (ad.rank <= 16) return launch_low<2>(ad, in, M, n_tok, width, low, st);
-    if (ad.rank <= 32) return launch_low<4>(ad, in, M, n_tok, width, low, st);
-    return launch_low<8>(ad, in, M, n_tok, width, low, st);
+  if (adapter_low_in_small_tiles(ad, n_tok)) {
+    if (ad.rank <= 8) return launch_low<1>(ad, in, M, n_tok, width, low, st, late);
+    if (ad.rank <= 16) return launch_low<2>(ad, in, M, n_tok, width, low, st, late);
+    if (ad.rank <= 32) return launch_low<4>(ad, in, M, n_tok, width, low, st, late);
+    return launch_low<8>(ad, in, M, n_tok, width, low, st, late);
   }
   return launch_low_tc(ad, in, M, n_tok, width, low, st);
 }

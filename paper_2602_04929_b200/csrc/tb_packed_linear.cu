@@ -23,15 +23,13 @@ tb_status adapter_low_simt(const Adapt& ad, const void* in, const void* M, tb_dt
 tb_status adapter_grad_simt(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low,
                             long long n_tok, int width, float* G, cudaStream_t st);
 
-tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low,
-                           cudaStream_t st);
 tb_status adapter_grad_bf16(const Adapt& ad, const void* in, const float* in_scales, const float* low, int n_tok, int width, float* G,
                             cudaStream_t st);
 
 static tb_status adapter_low(const Adapt& ad, const void* in, const void* M, tb_dtype type, long long n_tok, int width, float* low,
                              cudaStream_t st) {
   if (type == TB_BF16)
-    return adapter_low_bf16(ad, static_cast<const __nv_bfloat16*>(in), static_cast<const __nv_bfloat16*>(M), (int)n_tok, width, low, st);
+    return adapter_low_bf16(ad, static_cast<const __nv_bfloat16*>(in), static_cast<const __nv_bfloat16*>(M), (int)n_tok, width, low, false, st);
   return adapter_low_simt(ad, in, M, type, n_tok, width, low, st);
 }
 // of an input in `type`, or of 8-bit codes where their scales are given
@@ -106,16 +104,18 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
   return s;
 }
 
-static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out, const float* low,
+// in Q^T or in Q and the adapters' share, with their low = in M_i^T
+static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out, float* low,
                          bool back, void* ws, cudaStream_t st) {
+  if (type == TB_BF16 && !takes_few(type, n_tok, back))
+    return packed_product_tc(w, ad, static_cast<const __nv_bfloat16*>(in), n_tok, static_cast<__nv_bfloat16*>(out), low, back, ws, st);
+  if (ad.n) TB_TRY(adapter_low(ad, in, back ? ad.B : ad.A, type, n_tok, back ? w.d_out : w.d_in, low, st));
   if (takes_few(type, n_tok, back)) {
     PackedFew p;
     p.w = w, p.ad = ad, p.x = in, p.M = ad.B, p.low = low, p.out = out, p.n_tok = (int)n_tok;
     if (type == TB_BF16) return n_tok <= 8 ? packed_few_bf16_1(p, st) : packed_few_bf16_2(p, st);
     return n_tok <= 8 ? packed_few_f32_1(p, st) : packed_few_f32_2(p, st);
   }
-  if (type == TB_BF16)
-    return packed_product_tc(w, ad, static_cast<const __nv_bfloat16*>(in), n_tok, static_cast<__nv_bfloat16*>(out), low, back, ws, st);
   return packed_product_simt(w, ad, in, type, n_tok, out, low, back, st);
 }
 
@@ -142,7 +142,6 @@ extern "C" tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapte
   const Scratch sc = carve(pw, ad, x_type, n_tok, false, ws);
   if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
   cudaStream_t st = as_stream(stream);
-  if (ad.n) TB_TRY(adapter_low(ad, x, ad.A, x_type, n_tok, pw.d_in, xa, st));
   return product(pw, ad, x, x_type, n_tok, y, xa, false, sc.product, st);
 }
 
@@ -179,8 +178,10 @@ extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const 
   const Scratch sc = carve(pw, ad, x_type, n_tok, true, ws);
   if (sc.bytes && (!ws || !aligned(ws, 256) || ws_bytes < sc.bytes)) return TB_ERR_WORKSPACE;
   float* u = sc.u;
-  if (ad.n) TB_TRY(adapter_low(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
-  if (dx) TB_TRY(product(pw, ad, dy, x_type, n_tok, dx, u, true, sc.product, st));
+  if (dx)
+    TB_TRY(product(pw, ad, dy, x_type, n_tok, dx, u, true, sc.product, st));
+  else
+    TB_TRY(adapter_low(ad, dy, ad.B, x_type, n_tok, pw.d_out, u, st));
   if (dA) {
     TB_TRY(adapter_grad(ad, x_codes ? (const void*)x_codes : x, x_scales, x_type, u, n_tok, pw.d_in, dA, st));
     TB_TRY(adapter_grad(ad, dy, nullptr, x_type, xa, n_tok, pw.d_out, dB, st));

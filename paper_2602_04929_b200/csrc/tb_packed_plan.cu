@@ -180,7 +180,7 @@ static tb_status words_map(CUtensorMap* map, const unsigned* base, int words, in
 }
 
 tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat16* in, long long n_tok, __nv_bfloat16* out,
-                            const float* low, bool back, void* ws, cudaStream_t st) {
+                            float* low, bool back, void* ws, cudaStream_t st) {
   PackedTc p = {};
   p.n_cols = back ? w.d_in : w.d_out, p.n_sum = back ? w.d_out : w.d_in, p.n_tok = (int)n_tok;
   const TcPlan t = packed_tc_plan(p.n_tok, p.n_cols, p.n_sum);
@@ -202,12 +202,17 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   q.sz_ctas = q.sz_across * (p.rows_pad / 32);
   q.copy_ctas = q.copy ? (int)(((long long)w.d_out * p.pitch + 1023) / 1024) : 0;
   const dim3 prep((unsigned)(q.sz_ctas + q.copy_ctas + (p.n_runs ? t.t_tiles : 0)));
-  if (ad.n)  // beside the kernel that makes x A^T, which started when all before it had ended
+  // x A^T: before the product, which adds the adapters' share itself where the sum is not split; else beside it
+  const __nv_bfloat16* lowM = static_cast<const __nv_bfloat16*>(back ? ad.B : ad.A);
+  const bool late = ad.n && t.splits > 1 && adapter_low_in_small_tiles(ad, p.n_tok);
+  if (ad.n && !late) TB_TRY(adapter_low_bf16(ad, in, lowM, p.n_tok, p.n_sum, low, false, st));
+  if (ad.n && !late)  // beside that kernel, which started when all before it had ended
     TB_CUDA_CHECK(launch_pdl(k_packed_prep, prep, dim3(256), 0, st, q));
   else
     k_packed_prep<<<prep, 256, 0, st>>>(q);
   TB_LAUNCH_CHECK();
   TB_TRY(back ? packed_tc_backward(p, xmap, wmap, t.pairs, st) : packed_tc_forward(p, xmap, wmap, t.pairs, st));
+  if (late) TB_TRY(adapter_low_bf16(ad, in, lowM, p.n_tok, p.n_sum, low, true, st));
   if (t.splits > 1) {
     const long long n4 = (long long)p.n_tok * p.n_cols / 4;
     const long long nb = (n4 + 255) / 256;

@@ -191,6 +191,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     *odd_flag = 0;
     mbar_fence_init();
   }
+  if (threadIdx.x == 64) prefetch_map(&xmap), prefetch_map(&wmap);
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
