@@ -318,7 +318,7 @@ typedef struct {
   const int* zeros;           /* [d_out][n_g].  The quantizer's, 0 .. 2^bits - 1, and
                                  any in -128 .. 128 are exact; where code - zero
                                  needs more than bf16's eight bits, it is rounded
-                                 to about as many (not in dx of float activations) */
+                                 to about as many                                   */
 } tb_packed_weight;
 
 /* Low-rank adapters of the requests in a batch.  Request j has the tokens starts[j] ..

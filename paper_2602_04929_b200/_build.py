@@ -14,7 +14,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libturboboa.so")
 
 SOURCES = ["tb_api.cu", "tb_hessian.cu", "tb_syrk_tc.cu", "tb_syrk_tc2.cu", "tb_cross_tc.cu", "tb_gemm_tc.cu", "tb_i8.cu", "tb_factor.cu", "tb_factor_static.cu", "tb_quantize.cu", "tb_sweep.cu", "tb_grid_wide.cu", "tb_grid_digits.cu", "tb_cd_gram.cu", "tb_block.cu", "tb_pack.cu",
-           "tb_packed_linear.cu", "tb_packed_simt.cu", "tb_packed_plan.cu", "tb_packed_tc_fwd.cu", "tb_packed_tc_bwd.cu", "tb_adapters.cu",
+           "tb_packed_linear.cu", "tb_packed_f32.cu", "tb_adapters_f32.cu", "tb_packed_plan.cu", "tb_packed_tc_fwd.cu", "tb_packed_tc_bwd.cu", "tb_adapters.cu",
            "tb_packed_few_bf16_1.cu", "tb_packed_few_bf16_2.cu", "tb_packed_few_f32_1.cu", "tb_packed_few_f32_2.cu",
            "tb_checkpoint.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

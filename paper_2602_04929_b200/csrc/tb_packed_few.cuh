@@ -1,4 +1,4 @@
-// y = x Q^T for a few tokens (bf16), and for any number of them in float: mma.sync on weights decoded in registers.
+// y = x Q^T for a few tokens (up to 32 in bf16, 96 in float): mma.sync on weights decoded in registers.
 //
 // With few tokens the product is bound by reading the packed words and, at two to four bits, as much by the instructions that
 // decode them (logical operations go at half rate), so the words are

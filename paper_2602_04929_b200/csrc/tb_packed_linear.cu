@@ -16,12 +16,11 @@ int sm_count() {
   return count[dev];
 }
 
-tb_status packed_product_simt(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out,
-                              const float* low, bool back, cudaStream_t st);
-tb_status adapter_low_simt(const Adapt& ad, const void* in, const void* M, tb_dtype type, long long n_tok, int width, float* low,
-                           cudaStream_t st);
-tb_status adapter_grad_simt(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low,
-                            long long n_tok, int width, float* G, cudaStream_t st);
+tb_status packed_product_f32(const PackedW& w, const Adapt& ad, const float* in, int n_tok, float* out, const float* low, bool back,
+                             cudaStream_t st);
+tb_status adapter_low_f32(const Adapt& ad, const float* in, const float* M, long long n_tok, int width, float* low, cudaStream_t st);
+tb_status adapter_grad_f32(const Adapt& ad, const void* in, const float* in_scales, const float* low, long long n_tok, int width,
+                           float* G, cudaStream_t st);
 
 tb_status adapter_grad_bf16(const Adapt& ad, const void* in, const float* in_scales, const float* low, int n_tok, int width, float* G,
                             cudaStream_t st);
@@ -30,13 +29,13 @@ static tb_status adapter_low(const Adapt& ad, const void* in, const void* M, tb_
                              cudaStream_t st) {
   if (type == TB_BF16)
     return adapter_low_bf16(ad, static_cast<const __nv_bfloat16*>(in), static_cast<const __nv_bfloat16*>(M), (int)n_tok, width, low, false, st);
-  return adapter_low_simt(ad, in, M, type, n_tok, width, low, st);
+  return adapter_low_f32(ad, static_cast<const float*>(in), static_cast<const float*>(M), n_tok, width, low, st);
 }
 // of an input in `type`, or of 8-bit codes where their scales are given
 static tb_status adapter_grad(const Adapt& ad, const void* in, const float* in_scales, tb_dtype type, const float* low, long long n_tok,
                               int width, float* G, cudaStream_t st) {
   if (type == TB_BF16) return adapter_grad_bf16(ad, in, in_scales, low, (int)n_tok, width, G, st);
-  return adapter_grad_simt(ad, in, in_scales, type, low, n_tok, width, G, st);
+  return adapter_grad_f32(ad, in, in_scales, low, n_tok, width, G, st);
 }
 
 // Shapes first (so that the workspace queries can use them), pointers with `with_data`.
@@ -74,13 +73,15 @@ tb_status packed_few_bf16_2(const PackedFew& p, cudaStream_t st);
 tb_status packed_few_f32_1(const PackedFew& p, cudaStream_t st);
 tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
 
-// Which product: few tokens in bf16, and float whatever their number, read the weights into registers; more go to tcgen05 tiles, whose
-// smallest has 32 tokens.  The gradient of float inputs runs on the FP32 pipe.
+// Which product: for few tokens the weights go into registers; more bf16 tokens go to tcgen05 tiles, whose smallest has 32 tokens, more
+// float tokens, and the gradient of float inputs, to mma.sync tiles of 64.
 // Measured on 4096 x 4096, 4 bits / 8192 x 8192, 2 bits (us), registers / tiles: 24 tokens 13.9 / 17.1, 31.5 / 31.1; 32 tokens
 // 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.
-enum { FEW_TOKENS = 32 };
+// Float, 4 bits, registers / tiles: 4096 x 4096, 64 tokens 61 / 82, 128 tokens 104 / 82, 1024 tokens 784 / 585; 8192 x 8192, 128 tokens
+// 350 / 300, 1024 tokens 2740 / 2065; 1024 x 4096, 128 tokens 32 / 45, 256 tokens 60 / 46.
+enum { FEW_TOKENS = 32, FEW_TOKENS_F32 = 96 };
 static bool takes_few(tb_dtype type, long long n_tok, bool back) {
-  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= 65535ll * 16);
+  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= FEW_TOKENS_F32);
 }
 
 // Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.
@@ -116,7 +117,7 @@ static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_d
     if (type == TB_BF16) return n_tok <= 8 ? packed_few_bf16_1(p, st) : packed_few_bf16_2(p, st);
     return n_tok <= 8 ? packed_few_f32_1(p, st) : packed_few_f32_2(p, st);
   }
-  return packed_product_simt(w, ad, in, type, n_tok, out, low, back, st);
+  return packed_product_f32(w, ad, static_cast<const float*>(in), (int)n_tok, static_cast<float*>(out), low, back, st);
 }
 
 }  // namespace tb

@@ -490,3 +490,48 @@ def test_many_tiles_for_every_pair_of_processors(n_tok, rows, d, bits, group):
         # every token by itself: a rounding of its values, backward one of the weights too
         assert ((y - y64).norm(dim=1) <= 1.01 * 2.0 ** -8 * y64.norm(dim=1) + 1e-30).all()
         assert ((dx - dx64).norm(dim=1) <= 2.02 * 2.0 ** -8 * dx64.norm(dim=1) + 2.0 ** -8 * dy.double().norm(dim=1) * Q.norm(dim=1).max()).all()
+
+
+@pytest.mark.parametrize("group", [32, 128, 0])
+@pytest.mark.parametrize("n_tok", [3, 40, 97, 200])
+def test_what_is_not_finite_in_float(n_tok, group):
+    """Infinite and undefined activations stay with their token and become what the formula says; the largest floats stay finite."""
+    tb = _tb()
+    p = pu.problem(4, n_tok, 264, 256, 4, group, F32)
+    clean = p["x"].clone(), p["dy"].clone()
+    hit = torch.zeros(n_tok, dtype=torch.bool)
+    hit[:2] = True
+    p["x"][0, 17], p["x"][1, 200] = float("inf"), float("nan")
+    p["dy"][0, 30], p["dy"][1, 263] = float("-inf"), float("nan")
+    w, _ = pu.on_gpu(tb, p)
+    y, _ = tb.tb_packed_linear(w, p["x"].cuda())
+    dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    q = dict(p, x=clean[0], dy=clean[1])
+    want, _, bound = pu.forward64(q)
+    pu.near(y.cpu()[~hit], want[~hit], bound[~hit], "y")
+    ref = pu.backward64(q, None, None)["dx"]
+    pu.near(dx.cpu()[~hit], ref[0][~hit], ref[1][~hit], "dx")
+    Q = p["Q"]
+    for got, v, k in ((y, p["x"], Q.T), (dx, p["dy"], Q)):
+        got = got.cpu()
+        assert torch.isnan(got[1]).all()
+        at = int(torch.isinf(v[0]).nonzero()[0])
+        zero = k[at] == 0
+        assert torch.isnan(got[0][zero]).all()
+        assert torch.equal(got[0][~zero].double(), (v[0, at].double() * k[at])[~zero])
+
+
+@pytest.mark.parametrize("bits,group", [(4, 128), (4, 32), (7, 0)])
+@pytest.mark.parametrize("n_tok", [5, 130])
+def test_zero_points_outside_the_codes_in_float(bits, group, n_tok):
+    p = pu.problem(bits, n_tok, 136, 256, bits, group, F32)
+    z = torch.randint(-128, 129, p["zeros"].shape, generator=torch.Generator().manual_seed(bits), dtype=torch.int32)
+    wide = lambda v: v.double().repeat_interleave(p["d"] // v.shape[1], 1)  # noqa: E731
+    p["Q"] = p["Q"] + wide(p["zeros"] - z) * wide(p["scales"])
+    p["zeros"] = z
+    _forward(p)
+    tb = _tb()
+    w, _ = pu.on_gpu(tb, p)
+    dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    ref = pu.backward64(p, None, None)["dx"]
+    pu.near(dx, ref[0], ref[1], "dx")
