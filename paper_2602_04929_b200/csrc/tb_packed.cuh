@@ -35,19 +35,6 @@ __device__ __forceinline__ int adapter_of(const Adapt& a, long long t) {
   return id >= 0 && id < a.n ? id : -1;
 }
 
-// N codes from code j of a row on (j a multiple of 8, so the codes start on a byte), `row` its first word.
-template <int N>
-__device__ __forceinline__ void unpack_codes(const unsigned int* row, int words, int j, int bits, unsigned (&c)[N]) {
-  const unsigned mask = (1u << bits) - 1u;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int pos = (j + i) * bits, w = pos >> 5, s = pos & 31;
-    unsigned v = row[w] >> s;
-    if (s + bits > 32) v |= row[w + 1] << (32 - s);  // a code never crosses the end of its row
-    c[i] = v & mask;
-  }
-}
-
 // The input of a product of gradients: in full, or 8-bit codes with a scale for a token and CKPT_RUN columns.
 constexpr int CKPT_RUN = 128;
 

@@ -3,16 +3,17 @@
 //
 // A float is the sum of three bf16 pieces (all 24 bits), and c - z is exact in bf16, so three products with float sums lose nothing
 // that one in float would keep.  The scale is a row's and a run's of columns.  Forward, the contraction runs along the row: the sum of
-// a group is scaled when the group ends.  Backward it runs down the rows, so dy takes the scale before it is split, which needs a tile
+// a step is scaled.  Backward it runs down the rows, so dy takes the scale before it is split, which needs a tile
 // whose columns have one group: 32 columns (COLS) where groups are not multiples of 128.
 //
-// A step takes 32 of the contraction.  Activations are split and codes decoded once for the CTA, into shared memory (two buffers; rows
+// A step takes 32 of the contraction and its sum joins a float sum: the matrix instruction drops bits of its sum instead of rounding, so
+// long sums in it are off by 2^-24 of their size a step, all to one side.  Activations are split and codes decoded once for the CTA, into shared memory (two buffers; rows
 // padded so that ldmatrix meets no bank twice), while the step before is multiplied; the next step's words are on their way in
 // registers.  A cluster (cs CTAs) shares the contraction where tiles are few, and its sums are joined in a fixed order.  Adapters join
 // the finished sums on the FP32 pipe.
 //
-// 1024 tokens x 8192 x 8192, 4 bits: 2065 us forward, 200 TFLOP/s of bf16 products (a library's float product of that shape, without
-// the dequantizing, takes 2.2 ms); 4096 x 4096, 585 us.  It is bound by the load/store unit: fragments, split activations and codes
+// 1024 tokens x 8192 x 8192, 4 bits: 2128 us forward, 194 TFLOP/s of bf16 products (a library's float product of that shape, without
+// the dequantizing, takes 2.2 ms); 4096 x 4096, 603 us.  It is bound by the load/store unit: fragments, split activations and codes
 // pass through shared memory, and every row's words come in 8-byte pieces.
 #include "tb_packed_decode.cuh"
 #include "tb_packed.cuh"
@@ -158,11 +159,25 @@ __global__ void __launch_bounds__(F_THREADS, 2) k_packed_f32(PackedF32 p) {
 
   const int wm = warp / L::WN * (16 * MF), wn = warp % L::WN * (8 * NF);
   const int g = lane >> 2, q2 = 2 * (lane & 3);
-  float acc[MF][NF][4] = {}, sum[BACK ? 1 : MF][BACK ? 1 : NF][4] = {};
+  float acc[MF][NF][4], sum[MF][NF][4] = {}, row_scale[BACK ? 1 : NF][2];
   if (s0 < s1) fetch(s0), store(0);
   for (int s = s0; s < s1; ++s) {
     __syncthreads();  // this step's buffer is full, and nobody reads the other one
     if (s + 1 < s1) fetch(s + 1);
+#pragma unroll
+    for (int m = 0; m < MF; ++m)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) acc[m][f][0] = acc[m][f][1] = acc[m][f][2] = acc[m][f][3] = 0.0f;
+    if constexpr (!BACK)
+      if (s == s0 || s * F_K % w.group == 0) {  // a group begins
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int row = c0 + wn + 8 * f + q2 + j;
+            row_scale[f][j] = row < w.d_out ? w.scales[(long long)row * w.n_g + s * F_K / w.group] : 0.0f;
+          }
+      }
     const uint32_t a = base + (s - s0 & 1) * L::BUFFER, b = a + 3 * L::A_BYTES;
 #pragma unroll
     for (int kk = 0; kk < F_K; kk += 16) {
@@ -185,23 +200,17 @@ __global__ void __launch_bounds__(F_THREADS, 2) k_packed_f32(PackedF32 p) {
           for (int f = 0; f < NF; ++f) mma_f(acc[m][f], af, bf[f / 2][2 * (f & 1)], bf[f / 2][2 * (f & 1) + 1]);
         }
     }
-    if constexpr (!BACK) {
-      const int k1 = (s + 1) * F_K;
-      if (k1 % w.group == 0 || s + 1 == s1) {  // a group ends
 #pragma unroll
-        for (int f = 0; f < NF; ++f)
+    for (int m = 0; m < MF; ++m)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int row = c0 + wn + 8 * f + q2 + j;
-            const float sc = row < w.d_out ? w.scales[(long long)row * w.n_g + (k1 - 1) / w.group] : 0.0f;
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-            for (int m = 0; m < MF; ++m) {
-              sum[m][f][j] = fmaf(sc, acc[m][f][j], sum[m][f][j]), acc[m][f][j] = 0.0f;
-              sum[m][f][2 + j] = fmaf(sc, acc[m][f][2 + j], sum[m][f][2 + j]), acc[m][f][2 + j] = 0.0f;
-            }
-          }
-      }
-    }
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (BACK)
+            sum[m][f][j] += acc[m][f][j];
+          else
+            sum[m][f][j] = fmaf(row_scale[f][j & 1], acc[m][f][j], sum[m][f][j]);
+        }
     if (s + 1 < s1) store(s + 1 - s0 & 1);
   }
   __syncthreads();
@@ -212,12 +221,7 @@ __global__ void __launch_bounds__(F_THREADS, 2) k_packed_f32(PackedF32 p) {
     for (int f = 0; f < NF; ++f)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float2 r;
-        if constexpr (BACK)
-          r = make_float2(acc[m][f][2 * h], acc[m][f][2 * h + 1]);
-        else
-          r = make_float2(sum[m][f][2 * h], sum[m][f][2 * h + 1]);
-        *reinterpret_cast<float2*>(tile_sum + (wm + 16 * m + g + 8 * h) * L::S_PITCH + wn + 8 * f + q2) = r;
+        *reinterpret_cast<float2*>(tile_sum + (wm + 16 * m + g + 8 * h) * L::S_PITCH + wn + 8 * f + q2) = make_float2(sum[m][f][2 * h], sum[m][f][2 * h + 1]);
       }
   if (cs > 1)
     cluster_barrier();

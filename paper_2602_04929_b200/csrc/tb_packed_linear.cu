@@ -77,8 +77,8 @@ tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
 // float tokens, and the gradient of float inputs, to mma.sync tiles of 64.
 // Measured on 4096 x 4096, 4 bits / 8192 x 8192, 2 bits (us), registers / tiles: 24 tokens 13.9 / 17.1, 31.5 / 31.1; 32 tokens
 // 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.
-// Float, 4 bits, registers / tiles: 4096 x 4096, 64 tokens 61 / 82, 128 tokens 104 / 82, 1024 tokens 784 / 585; 8192 x 8192, 128 tokens
-// 350 / 300, 1024 tokens 2740 / 2065; 1024 x 4096, 128 tokens 32 / 45, 256 tokens 60 / 46.
+// Float, 4 bits, registers / tiles: 4096 x 4096, 64 tokens 61 / 85, 128 tokens 104 / 85, 1024 tokens 784 / 603; 8192 x 8192, 128 tokens
+// 350 / 309, 1024 tokens 2740 / 2128; 1024 x 4096, 128 tokens 32 / 46, 256 tokens 60 / 48.
 enum { FEW_TOKENS = 32, FEW_TOKENS_F32 = 96 };
 static bool takes_few(tb_dtype type, long long n_tok, bool back) {
   return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= FEW_TOKENS_F32);

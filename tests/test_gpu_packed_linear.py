@@ -535,3 +535,21 @@ def test_zero_points_outside_the_codes_in_float(bits, group, n_tok):
     dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
     ref = pu.backward64(p, None, None)["dx"]
     pu.near(dx, ref[0], ref[1], "dx")
+
+
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n_tok", [20, 100])
+def test_long_contractions_in_float(n_tok, group):
+    """Sums of 32 columns, in six (24 for few tokens: sums of 128) steps of the matrix unit that drop less than 2^-23 of a sum each, and 256
+    (64) float additions, each off by 2^-24 at most: in the mean of all values at most (2 * 24 + 8) 2^-24 or (2 * 6 + 16) 2^-24, since
+    the errors of different sums have nothing to do with one another.  (A warp's own sums in the kernel for few tokens are shorter.)"""
+    tb = _tb()
+    p = pu.problem(n_tok, n_tok, 8192, 8192, 4, group, F32)
+    w, _ = pu.on_gpu(tb, p)
+    y, _ = tb.tb_packed_linear(w, p["x"].cuda())
+    dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    Q = p["Q"].cuda()
+    tol = {True: 2 * 24 + 8, False: 2 * 6 + 16}
+    for got, v, k, few in ((y, p["x"], Q.T, n_tok <= 96), (dx, p["dy"], Q, False)):
+        want = v.cuda().double() @ k
+        assert float((got.double() - want).norm() / want.norm()) <= tol[few] * 2.0 ** -24
