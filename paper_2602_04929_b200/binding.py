@@ -586,8 +586,11 @@ def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=No
     n_tok, d_out = x.shape[0], w.widths[1]
     if y is None:
         y = x.new_empty((n_tok, d_out))
+        yp = y.data_ptr()
     elif tuple(y.shape) != (n_tok, d_out):
         raise ValueError("y must be [n_tok][d_out]")
+    else:
+        yp = _here(y, device, x.dtype)
     ap, xap, shape = None, None, None
     if adapters is None:
         xa = None
@@ -595,13 +598,14 @@ def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=No
         ap, shape = adapters.address, adapters.shape
         if xa is None:
             xa = x.new_empty((n_tok, shape[1]), dtype=torch.float32)
+            xap = xa.data_ptr()
         elif tuple(xa.shape) != (n_tok, shape[1]):
             raise ValueError("xa must be [n_tok][rank]")
-        xap = _here(xa, device, torch.float32)
-    lib = load()
+        else:
+            xap = _here(xa, device, torch.float32)
+    lib = _lib or load()
     wsp, wsb, keep = _scratch(lib.tb_packed_linear_workspace, w, ap, (0, xt, n_tok, shape), x, ws, device)
-    status = lib.tb_packed_linear(w.address, ap, _here(x, device, x.dtype), xt, n_tok, _here(y, device, x.dtype), xap, wsp, wsb,
-                                  _stream())
+    status = lib.tb_packed_linear(w.address, ap, _here(x, device, x.dtype), xt, n_tok, yp, xap, wsp, wsb, _stream())
     if status:
         raise TurboBoAError(status, "tb_packed_linear")
     return y, xa
