@@ -207,8 +207,9 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
   }
   const int room = AL_COLS / (p.n * p.n_parts), id0 = (int)blockIdx.y * room, ids = min(room, n_ids - id0);
   if (blockIdx.y == 0 && rank == 0)  // tokens without an adapter
-    for (int e = tid; e < AL_TOK * p.ad.rank; e += AL_THREADS)
-      if (own[e / p.ad.rank] == -1) p.low[(long long)t0 * p.ad.rank + e] = 0.0f;
+    for (int t = warp; t < AL_TOK; t += AL_THREADS / 32)
+      if (own[t] == -1)
+        for (int r = lane; r < p.ad.rank; r += 32) p.low[(long long)(t0 + t) * p.ad.rank + r] = 0.0f;
   if (ids <= 0) return;  // the same in every CTA of the cluster
   if (warp == 5) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((uint32_t)AL_COLS) : "memory");
@@ -264,40 +265,56 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
   __syncthreads();
   bool ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, &gave_up, &g_grad_error));
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  // a thread of the first four warps has a token, whose sums are in the columns of its adapter
   const uint32_t mine = smem_u32(sums);
-  const int pitch = p.n + 1, parts_here = (n_st + p.part - 1) / p.part;
-  for (int a = 0; a < ids; ++a) {
-    if (warp < 4)
-      for (int c = 0; c < p.n; c += 8) {
-        float v[8] = {};
-        for (int part = 0; part < parts_here && ok; ++part) {
-          uint32_t r[8];
-          tmem_ld_32x8(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)((a * p.n_parts + part) * p.n + c), r);
+  const int pitch = p.n + 1, parts_here = ok ? (n_st + p.part - 1) / p.part : 0;
+  if (warp < 4) {
+    bool here = false;
+    for (int a = 0; a < ids; ++a) {
+      const bool own_row = own[tid] == cand[id0 + a];
+      if (!__any_sync(0xffffffffu, own_row)) continue;
+      here = here || own_row;
+      for (int c = 0; c < p.n; c += 32) {
+        float v[32] = {};
+        for (int part = 0; part < parts_here; ++part) {
+          uint32_t r[4][8];
+#pragma unroll
+          for (int h = 0; h < 4; ++h)
+            if (c + 8 * h < p.n) tmem_ld_32x8(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)((a * p.n_parts + part) * p.n + c + 8 * h), r[h]);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(r[i]);
-        }
+          for (int h = 0; h < 4; ++h)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[tid * pitch + c + i] = v[i];
+            for (int i = 0; i < 8; ++i)
+              if (c + 8 * h < p.n) v[8 * h + i] += __uint_as_float(r[h][i]);
+        }
+        if (own_row)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (c + i < p.n) sums[tid * pitch + c + i] = v[i];
       }
-    __syncthreads();
-    if (cs > 1) cluster_barrier();
-    const int id = cand[id0 + a];
-    for (int e = tid + AL_THREADS * (int)rank; e < AL_TOK * p.ad.rank; e += AL_THREADS * (int)cs) {
-      const int t = e / p.ad.rank, r = e - t * p.ad.rank;
-      if (own[t] != id) continue;
-      float v = 0.0f;
-      for (uint32_t k = 0; k < cs; ++k) {
-        const float u = cs > 1 ? ld_cluster(map_to_rank(mine + 4u * (t * pitch + r), k)) : sums[t * pitch + r];
-        v = k ? v + u : u;
-      }
-      p.low[(long long)t0 * p.ad.rank + e] = v;
     }
-    if (cs > 1)
-      cluster_barrier();
-    else
-      __syncthreads();
+    if (!here) own[tid] = -2;  // of another CTA's adapters, or none
   }
+  if (cs > 1)
+    cluster_barrier();
+  else
+    __syncthreads();
+  for (int t = warp * (int)cs + (int)rank; t < AL_TOK; t += AL_THREADS / 32 * (int)cs) {  // a warp has a row
+    if (own[t] < 0) continue;
+    for (int r = lane; r < p.ad.rank; r += 32) {
+      float u[8];
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k)
+        u[k] = k >= cs ? 0.0f : cs > 1 ? ld_cluster(map_to_rank(mine + 4u * (t * pitch + r), k)) : sums[t * pitch + r];
+      float v = u[0];
+#pragma unroll
+      for (uint32_t k = 1; k < 8; ++k)
+        if (k < cs) v += u[k];
+      p.low[(long long)(t0 + t) * p.ad.rank + r] = v;
+    }
+  }
+  if (cs > 1) cluster_barrier();  // nobody leaves while its sums are read
   settle(*(volatile int*)&gave_up);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();

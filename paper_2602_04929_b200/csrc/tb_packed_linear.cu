@@ -73,15 +73,23 @@ tb_status packed_few_bf16_2(const PackedFew& p, cudaStream_t st);
 tb_status packed_few_f32_1(const PackedFew& p, cudaStream_t st);
 tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
 
-// Which product: for few tokens the weights go into registers; more bf16 tokens go to tcgen05 tiles, whose smallest has 32 tokens, more
-// float tokens, and the gradient of float inputs, to mma.sync tiles of 64.
+// Which product: where tokens are few or the work small, the weights go into registers (one launch instead of two or three); else bf16
+// goes to tcgen05 tiles, whose smallest has 32 tokens, and float, like the gradient of float inputs, to mma.sync tiles of 64.
 // Measured on 4096 x 4096, 4 bits / 8192 x 8192, 2 bits (us), registers / tiles: 24 tokens 13.9 / 17.1, 31.5 / 31.1; 32 tokens
-// 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.
+// 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.  Smaller weights, 4 bits (us in a graph): 2048 x 2048, 64 tokens
+// 9.1 / 12.5, 96 tokens 12.8 / 12.7; 1024 x 4096, 64 tokens 11.1 / 12.9, 96 tokens 15.9 / 12.6; 1024 x 1024, 128 tokens 6.9 / 10.9,
+// 256 tokens 9.3 / 11.8; 2048 x 512, 128 tokens 7.9 / 9.7, 256 tokens 14.5 / 10.3; 512 x 512, 512 tokens 7.9 / 9.5, 1023 tokens 14.3 /
+// 10.2.  The adapters' share is computed per 16 tokens here: rank 16, 1024 x 1024, 256 tokens 18.4 / 20.5; rank 64, 512 x 512, 128
+// tokens 19.1 / 44, 512 tokens 35.7 / 32.6; rank 128, 512 x 512, 64 tokens 14.7 / 33.4, 256 tokens 36.0 / 32.7, 8192 x 512, 64 tokens
+// 100 / 35.
 // Float, 4 bits, registers / tiles: 4096 x 4096, 64 tokens 61 / 85, 128 tokens 104 / 85, 1024 tokens 784 / 603; 8192 x 8192, 128 tokens
 // 350 / 309, 1024 tokens 2740 / 2128; 1024 x 4096, 128 tokens 32 / 46, 256 tokens 60 / 48.
-enum { FEW_TOKENS = 32, FEW_TOKENS_F32 = 96 };
-static bool takes_few(tb_dtype type, long long n_tok, bool back) {
-  return !back && (type == TB_BF16 ? n_tok <= FEW_TOKENS : n_tok <= FEW_TOKENS_F32);
+enum { FEW_TOKENS = 32, FEW_TOKENS_F32 = 96, FEW_OUTPUTS = 1 << 18, FEW_WORK = 1 << 28 };
+static bool takes_few(const PackedW& w, const Adapt& ad, tb_dtype type, long long n_tok, bool back) {
+  if (back) return false;
+  if (type == TB_F32) return n_tok <= FEW_TOKENS_F32;
+  const long long outputs = n_tok * w.d_out, ranks = ad.n && ad.rank > 16 ? ad.rank : 16;  // n_tok < 2^30, d_out <= 2^24
+  return n_tok <= FEW_TOKENS || (outputs * ranks <= FEW_OUTPUTS * 16ll && outputs * w.d_in <= FEW_WORK);
 }
 
 // Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.
@@ -95,10 +103,10 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
   Bump b(ws);
   s.u = back && ad.n ? b.take<float>((size_t)n_tok * ad.rank) : nullptr;
   size_t n = 0;
-  if (type == TB_BF16 && !takes_few(type, n_tok, back)) {
+  if (type == TB_BF16 && !takes_few(w, ad, type, n_tok, back)) {
     PackedTc p;
     const int cols = back ? w.d_in : w.d_out;
-    n = packed_tc_carve(packed_tc_plan((int)n_tok, cols, back ? w.d_out : w.d_in), w, ad, (int)n_tok, cols, back, nullptr, &p);
+    n = packed_tc_carve(packed_tc_plan(ad, (int)n_tok, cols, back ? w.d_out : w.d_in), w, ad, (int)n_tok, cols, back, nullptr, &p);
   }
   s.product = b.take<char>(n);
   s.bytes = (back && ad.n) || n ? b.total() : 0;
@@ -108,10 +116,10 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
 // in Q^T or in Q and the adapters' share, with their low = in M_i^T
 static tb_status product(const PackedW& w, const Adapt& ad, const void* in, tb_dtype type, long long n_tok, void* out, float* low,
                          bool back, void* ws, cudaStream_t st) {
-  if (type == TB_BF16 && !takes_few(type, n_tok, back))
+  if (type == TB_BF16 && !takes_few(w, ad, type, n_tok, back))
     return packed_product_tc(w, ad, static_cast<const __nv_bfloat16*>(in), n_tok, static_cast<__nv_bfloat16*>(out), low, back, ws, st);
   if (ad.n) TB_TRY(adapter_low(ad, in, back ? ad.B : ad.A, type, n_tok, back ? w.d_out : w.d_in, low, st));
-  if (takes_few(type, n_tok, back)) {
+  if (takes_few(w, ad, type, n_tok, back)) {
     PackedFew p;
     p.w = w, p.ad = ad, p.x = in, p.M = ad.B, p.low = low, p.out = out, p.n_tok = (int)n_tok;
     if (type == TB_BF16) return n_tok <= 8 ? packed_few_bf16_1(p, st) : packed_few_bf16_2(p, st);

@@ -120,8 +120,10 @@ __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* 
 
 // Tile and splits by an estimate of the clocks, fitted to sweeps of both (64 to 1999 tokens, widths of 1024 to 8192): a stage of 64
 // columns costs its decoding, whatever the tile, and a little for every token, a tile 1500 clocks and what its results take, and
-// splits cost writing and adding their float sums.
-TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
+// splits cost writing and adding their float sums.  The adapters' share is further stages of the tile, four slots each (see the
+// kernel), or joins the float sums: 64 tokens of 32 requests, rank 64, 8192 x 512, has 64 such stages and takes 70 us with them, TODO us
+// joined.
+TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum) {
   TcPlan best = {};
   double best_cost = 0.0;
   int sms = sm_count();
@@ -137,12 +139,21 @@ TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum) {
       if (tiles > 0x3fffffff) continue;
       const double waves = (double)((tiles + pairs - 1) / pairs);
       const double stage = 600.0 + 0.4 * n_tile;
-      double cost = waves * (len / 64 * stage + 1500.0 + 6.0 * n_tile);
-      if (splits > 1) cost += 4000.0 + 8.0 * splits * (double)n_tok * n_cols / 2500.0;
-      if (best.n_tile == 0 || cost < best_cost) {
-        best_cost = cost;
-        best.n_tile = n_tile, best.m_tiles = m_tiles, best.t_tiles = t_tiles, best.splits = splits, best.split_len = len;
-        best.pairs = tiles < pairs ? (int)tiles : pairs;
+      const double plain = waves * (len / 64 * stage + 1500.0 + 6.0 * n_tile);
+      for (int joined = splits > 1; joined <= (splits > 1 || ad.n); ++joined) {
+        double cost = plain;
+        if (joined) {
+          cost += 4000.0 + 8.0 * splits * (double)n_tok * n_cols / 2500.0;
+          if (ad.n) cost += 2000.0 + (double)n_tok * n_cols * ad.rank / 2600.0;
+        } else if (ad.n) {
+          const double runs = min((double)min(n_tile, ad.n_req), 1.0 + (double)ad.n_req * n_tile / n_tok);
+          cost += waves * (3000.0 + 1600.0 * ceil(runs * ((ad.rank + 15) / 16) * 2.0 / 4.0));
+        }
+        if (best.n_tile == 0 || cost < best_cost) {
+          best_cost = cost;
+          best.n_tile = n_tile, best.m_tiles = m_tiles, best.t_tiles = t_tiles, best.splits = splits, best.split_len = len;
+          best.pairs = tiles < pairs ? (int)tiles : pairs, best.joined = joined;
+        }
       }
     }
   }
@@ -156,9 +167,9 @@ size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n
   p->st = back ? nullptr : b.take<float>((size_t)w.n_g * p->rows_pad);
   p->zt = b.take<unsigned>((size_t)w.n_g * p->rows_pad * (back ? 2 : 1));
   p->words = p->pitch != w.words ? b.take<unsigned>((size_t)w.d_out * p->pitch) : w.packed;
-  p->runs = ad.n && t.splits == 1 ? b.take<int4>(n_tok) : nullptr;
-  p->n_runs = ad.n && t.splits == 1 ? b.take<int>(t.t_tiles) : nullptr;
-  p->part = t.splits > 1 ? b.take<float>((size_t)t.splits * n_tok * n_cols) : nullptr;
+  p->runs = ad.n && !t.joined ? b.take<int4>(n_tok) : nullptr;
+  p->n_runs = ad.n && !t.joined ? b.take<int>(t.t_tiles) : nullptr;
+  p->part = t.joined ? b.take<float>((size_t)t.splits * n_tok * n_cols) : nullptr;
   return b.total();
 }
 
@@ -183,7 +194,7 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
                             float* low, bool back, void* ws, cudaStream_t st) {
   PackedTc p = {};
   p.n_cols = back ? w.d_in : w.d_out, p.n_sum = back ? w.d_out : w.d_in, p.n_tok = (int)n_tok;
-  const TcPlan t = packed_tc_plan(p.n_tok, p.n_cols, p.n_sum);
+  const TcPlan t = packed_tc_plan(ad, p.n_tok, p.n_cols, p.n_sum);
   packed_tc_carve(t, w, ad, p.n_tok, p.n_cols, back, static_cast<char*>(ws), &p);
   p.w = w, p.ad = ad, p.low = low, p.out = out;
   p.M = static_cast<const __nv_bfloat16*>(back ? ad.A : ad.B);
@@ -202,9 +213,9 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   q.sz_ctas = q.sz_across * (p.rows_pad / 32);
   q.copy_ctas = q.copy ? (int)(((long long)w.d_out * p.pitch + 1023) / 1024) : 0;
   const dim3 prep((unsigned)(q.sz_ctas + q.copy_ctas + (p.n_runs ? t.t_tiles : 0)));
-  // x A^T: before the product, which adds the adapters' share itself where the sum is not split; else beside it
+  // x A^T: before the product, which adds the adapters' share itself where its sums are not joined; else beside it
   const __nv_bfloat16* lowM = static_cast<const __nv_bfloat16*>(back ? ad.B : ad.A);
-  const bool late = ad.n && t.splits > 1 && adapter_low_in_small_tiles(ad, p.n_tok);
+  const bool late = ad.n && t.joined && adapter_low_in_small_tiles(ad, p.n_tok);
   if (ad.n && !late) TB_TRY(adapter_low_bf16(ad, in, lowM, p.n_tok, p.n_sum, low, false, st));
   if (ad.n && !late)  // beside that kernel, which started when all before it had ended
     TB_CUDA_CHECK(launch_pdl(k_packed_prep, prep, dim3(256), 0, st, q));
@@ -213,7 +224,7 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
   TB_LAUNCH_CHECK();
   TB_TRY(back ? packed_tc_backward(p, xmap, wmap, t.pairs, st) : packed_tc_forward(p, xmap, wmap, t.pairs, st));
   if (late) TB_TRY(adapter_low_bf16(ad, in, lowM, p.n_tok, p.n_sum, low, true, st));
-  if (t.splits > 1) {
+  if (t.joined) {
     const long long n4 = (long long)p.n_tok * p.n_cols / 4;
     const long long nb = (n4 + 255) / 256;
     TB_CUDA_CHECK(launch_pdl(k_packed_join, dim3((unsigned)(nb < 4096 ? nb : 4096)), dim3(256), 0, st, reinterpret_cast<const float4*>(p.part),

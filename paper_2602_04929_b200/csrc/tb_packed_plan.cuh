@@ -27,14 +27,15 @@ struct PackedTc {
   const int4* runs;        // per token tile, from its first token's index on: first token, end, adapter
   const int* n_runs;       // per token tile; nullptr: no adapters, or added with the splits' sums
   __nv_bfloat16* out;      // [n_tok][n_cols]
-  float* part;             // splits > 1: [split][n_tok][n_cols]
+  float* part;             // [split][n_tok][n_cols] where the sums are joined afterwards, else nullptr
   int n_tok, n_cols, n_sum, n_tile, m_tiles, t_tiles, splits, split_len;
 };
 
 struct TcPlan {
   int n_tile, m_tiles, t_tiles, splits, split_len, pairs;
+  bool joined;  // float sums, added with the adapters' share by a kernel of their own: with splits, or where runs are many
 };
-TcPlan packed_tc_plan(int n_tok, int n_cols, int n_sum);
+TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum);
 // Scratch of a product from `ws` on (nullptr: only its size).
 size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, bool back, char* ws, PackedTc* p);
 // out = in Q^T or in Q, with the adapters' share; makes their low [n_tok][rank] = in M_i^T too.

@@ -593,7 +593,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           tmem_ld_32x16(taddr + ch * 16, r);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
           if (!store) continue;
-          if (p.splits > 1) {
+          if (p.part) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (16 * ch + i < n) fo[(16 * ch + i) * p.n_cols] = __uint_as_float(r[i]);
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
         }
         if (!ok) break;
         if (store) {
-          if (p.splits > 1) {
+          if (p.part) {
 #pragma unroll
             for (int i = 0; i < 128; ++i)
               if (i < n) fo[i * p.n_cols] = run[i];

@@ -50,6 +50,15 @@ def test_shapes_float(rows, d, group, n_tok):
     _forward(pu.problem(rows + d, n_tok, rows, d, 2, group, F32), (rows, d, group, n_tok))
 
 
+@pytest.mark.parametrize("rows,d,group,bits", [(8, 32, 0, 4), (24, 32, 32, 3), (136, 96, 96, 5), (264, 160, 32, 2), (128, 544, 0, 6), (1032, 128, 64, 4),
+                                               (256, 1024, 256, 7), (520, 1152, 384, 8), (16, 2080, 416, 3), (2056, 640, 128, 2)])
+@pytest.mark.parametrize("more", [1, 31, 200])
+def test_shapes_in_tiles(rows, d, group, bits, more):
+    """As many tokens as go to the tensor-core tiles: more than 2^18 results."""
+    n_tok = (1 << 18) // rows + more
+    _forward(pu.problem(rows + d, n_tok, rows, d, bits, group, BF), (rows, d, group, n_tok))
+
+
 REQUESTS = {
     "one": (40, [0, 40], [0]),
     "single tokens": (11, list(range(12)), [3, 1, 1, -1, 0, 2, 3, 9, 0, 0, 1]),
@@ -71,6 +80,16 @@ def _with_adapters(name, rank, dtype, rows=264, d=416, bits=4, group=32):
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_adapters(name, rank, dtype):
     _forward(_with_adapters(name, rank, dtype), name)
+
+
+@pytest.mark.parametrize("n_tok,rows,d,n_req,rank", [(64, 2056, 512, 32, 64), (70, 2056, 256, 70, 16), (1100, 264, 416, 3, 8), (1100, 264, 416, 1100, 8),
+                                                   (300, 1032, 256, 5, 128), (300, 1032, 1024, 300, 128), (2100, 136, 96, 9, 32)])
+def test_adapters_in_tiles(n_tok, rows, d, n_req, rank):
+    """Requests in the tiles' own stages and joined to their sums, many and few of them."""
+    g = torch.Generator().manual_seed(n_tok + rows)
+    cuts = torch.sort(torch.randint(0, n_tok + 1, (n_req - 1,), generator=g)).values.tolist()
+    starts = list(range(n_tok + 1)) if n_req == n_tok else [0, *cuts, n_tok]
+    _forward(pu.problem(7, n_tok, rows, d, 4, 32, BF, 5, rank, starts, torch.randint(-1, 5, (n_req,), generator=g).tolist()))
 
 
 @pytest.mark.parametrize("name", REQUESTS)
@@ -451,7 +470,7 @@ def test_refusals():
             call()
             pytest.fail(f"call {k} was taken")
     both = tb.tb_checkpoint_pack(x)
-    for call, status in ((lambda: tb.tb_packed_linear(w, x, a, ws=torch.empty(256, dtype=torch.uint8, device="cuda")), 3),
+    for call, status in ((lambda: tb.tb_packed_linear_backward(w, dy, a, x=x, xa=xa, ws=torch.empty(256, dtype=torch.uint8, device="cuda")), 3),
                          (lambda: tb.tb_packed_linear_backward(w, dy, a, x=x, checkpoint=both, xa=xa), 1),
                          (lambda: tb.tb_packed_linear_backward(w, dy, want_dx=False), 1)):
         with pytest.raises(tb.TurboBoAError) as e:
@@ -461,6 +480,10 @@ def test_refusals():
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     y, _ = tb.tb_packed_linear(w, x, a, ws=ws)
     assert torch.equal(y, tb.tb_packed_linear(w, x, a)[0])
+    need = tb.load().tb_packed_linear_backward_workspace(w.address, a.address, 1, 40)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    got = tb.tb_packed_linear_backward(w, dy, a, x=x, xa=xa, ws=ws)
+    assert all(torch.equal(u, v) for u, v in zip(got, tb.tb_packed_linear_backward(w, dy, a, x=x, xa=xa)))
 
 
 @pytest.mark.parametrize("n_tok,rows,d,bits,group", [(20000, 40, 520 - 8, 2, 0), (9000, 264, 96, 3, 96), (33000, 8, 160, 7, 32), (5000, 1032, 1056, 4, 0)])
