@@ -145,10 +145,13 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
 
 // The same for many tokens, on tcgen05: 128 tokens are the rows M of the tile, the rank its columns N, both operands by TMA as they
 // are stored (K-major).  x so is read once, at HBM's rate, and an adapter once for 128 tokens.  A tile's adapters (AL_COLS / N of
-// them, more in further CTAs) are gone through one after the other, each into columns of its own; rows of other adapters are computed and dropped.
-// CTAs of a cluster share the contraction; an accumulation ends after 512 columns where tensor memory has room for more of them (every step may drop the last bit).
+// them, more in further CTAs) are gone through one after the other, each into columns of its own; rows of other adapters are computed and
+// dropped.  CTAs of a cluster share the contraction; an accumulation ends after 512 columns where tensor memory has room for more of
+// them (every step may drop the last bit).
+//
+// 8192 x 4096, rank 16: 22 us (67 MB at 3.0 TB/s); 4099 x 8192, rank 64: 33 us (67 MB at 2.0 TB/s).  A tile is loaded, multiplied and
+// written by one CTA an SM in turn, so that neither end of it overlaps with another tile's loads.
 
-enum { LOW_TC_WORK = 65536 };  // tokens x rank
 enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_PART = 512, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
 
 struct LowTc {
@@ -365,17 +368,19 @@ static tb_status launch_low_tc(const Adapt& ad, const __nv_bfloat16* in, const _
 }
 
 // Tiles of 16 tokens start sooner and compute less for rows of other adapters, but read an adapter once for every 16 tokens.
-// Measured, tiles of 16 / tcgen05: 512 x 4096, rank 16, 6.4 / 8.6 us; 1999 x 4096, rank 32, 23 requests, 13.9 / 17.6 us;
-// 1024 x 8192, rank 64, 29 / 20 us; 4099 x 8192, rank 64, 68 (tiles of 64) / 36 us.
-bool adapter_low_in_small_tiles(const Adapt& ad, int n_tok) {
-  return (long long)n_tok * ad.rank < LOW_TC_WORK || (long long)n_tok / ad.n_req < 48;
+// Measured, tiles of 16 / tcgen05 (us): rank 128, 4 requests, 512 x 256 7.6 / 23.7, 512 x 1024 10.2 / 16.0, 512 x 4096 25.7 / 16.2, 1024 x
+// 4096 18.8 / 16.4; rank 64, 1024 x 1024 9.0 / 12.2, 2048 x 2048 15.1 / 18.5, 4096 x 1024 12.3 / 12.5, 1024 x 4096 17.2 / 13.3, 1024 x 8192
+// 44 / 18; rank 16, 4096 x 4096 14.1 / 17.0.  Where requests are short, most rows of a tile of 128 are another adapter's.
+enum { LOW_TC_WORK = 1 << 28 };  // tokens x rank x width
+bool adapter_low_in_small_tiles(const Adapt& ad, int n_tok, int width) {
+  return (long long)n_tok * ad.rank * width < LOW_TC_WORK || n_tok / ad.n_req < 48;  // n_tok < 2^30, rank <= 2^7, width <= 2^24
 }
 
 // low [n_tok][rank] = in M_i^T for the adapter i of every token, zero for a token without one.  `late` (small tiles only): the call
 // before on the stream is a product that does not need it, and the one after waits for both.
 tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, bool late,
                            cudaStream_t st) {
-  if (adapter_low_in_small_tiles(ad, n_tok)) {
+  if (adapter_low_in_small_tiles(ad, n_tok, width)) {
     if (ad.rank <= 8) return launch_low<1>(ad, in, M, n_tok, width, low, st, late);
     if (ad.rank <= 16) return launch_low<2>(ad, in, M, n_tok, width, low, st, late);
     if (ad.rank <= 32) return launch_low<4>(ad, in, M, n_tok, width, low, st, late);

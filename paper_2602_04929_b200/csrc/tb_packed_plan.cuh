@@ -41,7 +41,7 @@ size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n
 // out = in Q^T or in Q, with the adapters' share; makes their low [n_tok][rank] = in M_i^T too.
 tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat16* in, long long n_tok, __nv_bfloat16* out,
                             float* low, bool back, void* ws, cudaStream_t st);
-bool adapter_low_in_small_tiles(const Adapt& ad, int n_tok);
+bool adapter_low_in_small_tiles(const Adapt& ad, int n_tok, int width);
 tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, bool late,
                            cudaStream_t st);
 tb_status packed_tc_forward(const PackedTc& p, const CUtensorMap& xmap, const CUtensorMap& wmap, int pairs, cudaStream_t st);

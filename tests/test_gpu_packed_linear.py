@@ -576,3 +576,12 @@ def test_long_contractions_in_float(n_tok, group):
     for got, v, k, few in ((y, p["x"], Q.T, n_tok <= 96), (dx, p["dy"], Q, False)):
         want = v.cuda().double() @ k
         assert float((got.double() - want).norm() / want.norm()) <= tol[few] * 2.0 ** -24
+
+
+@pytest.mark.parametrize("n_tok,d,n_req,rank", [(22000, 96, 5, 128), (9000, 416, 150, 80), (3001, 1184, 60, 128), (17000, 2080, 3, 8), (2100, 1056, 1, 128)])
+def test_narrow_product_in_tiles(n_tok, d, n_req, rank):
+    g = torch.Generator().manual_seed(n_tok)
+    starts = [3, *torch.sort(torch.randint(3, n_tok - 5, (n_req - 1,), generator=g)).values.tolist(), n_tok - 5]
+    ids = torch.randint(-1, 7, (n_req,), generator=g).tolist()
+    ids[-1] = 2
+    _forward(pu.problem(7, n_tok, 40, d, 4, 32, BF, 7, rank, starts, ids))
