@@ -15,6 +15,9 @@
 // leave a CTA and a half for every SM; where even 16 rows do not, CTAs of a cluster (cs of them) have a range of blocks each.  The
 // warps' and the CTAs' sums are joined in a fixed order.
 //
+// 1 token: 4096 x 4096, 4 bits, 6.0 us; 8192 x 8192, 2 bits, 13.0 us (17 MB of words and 4 MB of scales, 1.6 TB/s); 64 tokens x 2048 x
+// 2048, 4 bits, 9.1 us.  Decoding bounds it, an instruction for every two codes at half rate, after about 3 us of launch and first loads.
+//
 // NARROW: scales of fewer than 128 columns, or a width that is no multiple of 128.  A lane then takes 8 codes of a run of 32.
 #pragma once
 
