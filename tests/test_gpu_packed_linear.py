@@ -585,3 +585,43 @@ def test_narrow_product_in_tiles(n_tok, d, n_req, rank):
     ids = torch.randint(-1, 7, (n_req,), generator=g).tolist()
     ids[-1] = 2
     _forward(pu.problem(7, n_tok, 40, d, 4, 32, BF, 7, rank, starts, ids))
+
+
+@pytest.mark.parametrize("n_tok,rows,d,rank,dtype", [(24, 264, 512, 16, BF), (70, 4104, 1024, 64, BF), (400, 1032, 768, 32, BF), (2300, 264, 1056, 128, BF), (130, 264, 512, 16, F32)])
+def test_calls_one_after_the_other_and_side_by_side(n_tok, rows, d, rank, dtype):
+    """Calls that take the same outputs and scratch in turn, and calls of two streams at once, give the bits of a call by itself."""
+    tb = _tb()
+    n_req = 5
+    cuts = torch.sort(torch.randint(0, n_tok + 1, (n_req - 1,), generator=torch.Generator().manual_seed(n_tok))).values.tolist()
+    p = pu.problem(n_tok, n_tok, rows, d, 4, 32, dtype, 3, rank, [0, *cuts, n_tok], [0, 2, 1, 0, 2])
+    w, a = pu.on_gpu(tb, p)
+    xs = [p["x"].cuda() * s for s in (1.0, -2.0, 0.5, 4.0)]
+    dys = [p["dy"].cuda() * s for s in (1.0, 0.5, -2.0, 1.0)]
+
+    def one(x, dy, **kept):
+        y, xa = tb.tb_packed_linear(w, x, a, **kept)
+        dx, dA, dB = tb.tb_packed_linear_backward(w, dy, a, x=x, xa=xa, ws=kept.get("ws"))
+        return [v.clone() for v in (y, xa, dx, dA, dB)]
+
+    alone = []
+    for x, dy in zip(xs, dys):
+        alone.append(one(x, dy))
+        torch.cuda.synchronize()
+    lib, t = tb.load(), {BF: 1, F32: 0}[dtype]
+    need = max(lib.tb_packed_linear_workspace(w.address, a.address, t, n_tok), lib.tb_packed_linear_backward_workspace(w.address, a.address, t, n_tok))
+    kept = dict(ws=torch.empty(need, dtype=torch.uint8, device="cuda"), y=torch.empty_like(alone[0][0]), xa=torch.empty_like(alone[0][1]))
+    for _ in range(5):
+        got = [one(x, dy, **kept) for x, dy in zip(xs, dys)]
+        assert all(torch.equal(u, v) for g, s in zip(got, alone) for u, v in zip(g, s))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for k in range(12):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(one(xs[(k + i) % 4], dys[(k + i) % 4]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for k in range(12):
+            assert all(torch.equal(u, v) for u, v in zip(got[i][k], alone[(k + i) % 4])), (i, k)
+    assert tb.tb_device_error_flag() == 0
