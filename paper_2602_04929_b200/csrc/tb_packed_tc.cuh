@@ -386,7 +386,10 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
         const int n_u = BACK ? (c.k1 - c.k0 + 63) / 64 : (c.k1 - c.k0 + 127) / 128;
-        int r = BACK ? c.k0 : c.m0, j = BACK ? c.m0 : c.k0, g = (j >> 5) / G, left = (g + 1) * G - (j >> 5);
+        int r = BACK ? c.k0 : c.m0, j = BACK ? c.m0 : c.k0;
+        // (backward, the second CTA's columns may all lie behind the matrix: any zero-points will do for them)
+        const int g = min(j >> 5, last) / G;
+        int left = (g + 1) * G - (j >> 5);
         const unsigned* zt = p.zt + ((long long)g * p.rows_pad + r) * (BACK ? 2 : 1);  // of the unit's first run
         for (int u = 0; u < n_u; ++u) {
           ok = mbar_wait(raw_empty(s), phase, abort_flag, &g_packed_error);

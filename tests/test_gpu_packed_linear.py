@@ -625,3 +625,46 @@ def test_calls_one_after_the_other_and_side_by_side(n_tok, rows, d, rank, dtype)
         for k in range(12):
             assert all(torch.equal(u, v) for u, v in zip(got[i][k], alone[(k + i) % 4])), (i, k)
     assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("n_tok,rows,d,bits,group,rank", [(208, 832, 2688, 4, 128, 128), (40, 136, 384, 4, 128, 8), (300, 1160, 128, 3, 0, 16), (70, 264, 640, 8, 128, 8),
+                                                        (1100, 264, 384, 2, 384, 8), (90, 200, 96, 5, 96, 16), (24, 136, 1152, 7, 128, 16), (1, 8, 32, 2, 32, 8)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_inputs_and_scratch_that_end_with_their_memory(n_tok, rows, d, bits, group, rank, dtype):
+    """Every array at the very end of an allocation of its own: nothing behind it is read (columns of a tile behind the matrix, for
+    instance, whose zero-points no group has)."""
+    tb = _tb()
+    hold = []
+
+    def at_the_end(v):
+        n = v.numel() * v.element_size()
+        room = torch.empty(max(16 << 20, (n + (2 << 20) - 1) >> 21 << 21), dtype=torch.uint8, device="cuda")
+        hold.append(room)
+        to = room[(room.numel() - n) // 256 * 256:][:n].view(v.dtype).view(v.shape)
+        to.copy_(v)
+        return to
+
+    p = pu.problem(n_tok + rows, n_tok, rows, d, bits, group, dtype, 2, rank, sorted([0, n_tok // 3, n_tok // 2, n_tok]), [1, 0, 1])
+    w0, a0 = pu.on_gpu(tb, p)
+    w = tb.packed_weight(*(at_the_end(v) for v in w0.tensors), d, bits, group)
+    a = tb.adapters(*(at_the_end(v) for v in a0.tensors))
+    x, dy = at_the_end(p["x"].cuda()), at_the_end(p["dy"].cuda())
+    lib, t = tb.load(), {BF: 1, F32: 0}[dtype]
+
+    def scratch(size):
+        return at_the_end(torch.zeros(max(256, (size + 255) // 256 * 256), dtype=torch.uint8, device="cuda"))
+
+    y, xa = tb.tb_packed_linear(w, x, a, ws=scratch(lib.tb_packed_linear_workspace(w.address, a.address, t, n_tok)))
+    want, xa64, bound = pu.forward64(p)
+    pu.near(y, want, bound, "y")
+    plain, _ = tb.tb_packed_linear(w, x, None, ws=scratch(lib.tb_packed_linear_workspace(w.address, None, t, n_tok)))
+    assert torch.isfinite(plain).all()
+    codes, scales = (at_the_end(v) for v in tb.tb_checkpoint_pack(x))
+    assert torch.isfinite(tb.tb_checkpoint_unpack(codes, scales, dtype)).all()
+    xa = at_the_end(xa)
+    ref = pu.backward64(p, None, xa.cpu())
+    for kept in (dict(x=x), dict(checkpoint=(codes, scales))):
+        dx, dA, dB = tb.tb_packed_linear_backward(w, dy, a, xa=xa, ws=scratch(lib.tb_packed_linear_backward_workspace(w.address, a.address, t, n_tok)), **kept)
+        pu.near(dx, ref["dx"][0], ref["dx"][1], "dx")
+        pu.near(dB, ref["dB"][0], ref["dB"][1], "dB")
+    assert tb.tb_device_error_flag() == 0
