@@ -21,11 +21,11 @@ static __device__ int g_grad_error = 0;
 
 // ------------------------------------------------------------------------------------------ x A_i^T
 //
-// For few tokens, on mma.sync: a CTA has 16 tokens, one of the adapters that they have, up to 64 of its rank and, as one of a
-// cluster, a share of the contraction, which its warps split further.  Operands go from global memory straight into fragments: a lane loads 16 bytes of a row, eight neighbouring columns, and which columns a fragment
-// calls k = 0 .. 15 does not matter as long as both operands agree.  Rows of other adapters are not read.  The warps' and the CTAs'
-// sums are added in a fixed order.  8 tokens x 8192, rank 8: 5.7 us, latency; 1999 x 4096, rank 32: 17 us (16 MB of x, 1.0 TB/s; the
-// adapters come from L2 once for every 16 tokens).
+// For few tokens, on mma.sync: a CTA has 16 tokens, one of the adapters that they have, up to 64 of its rank and, as one of a cluster,
+// a share of the contraction, which its warps split further.  Operands go from global memory straight into fragments: a lane loads 16
+// bytes of a row, eight neighbouring columns, and which columns a fragment calls k = 0 .. 15 does not matter as long as both operands
+// agree.  Rows of other adapters are not read.  The warps' and the CTAs' sums are added in a fixed order.  8 tokens x 8192, rank 8: 5.7
+// us, latency; 1999 x 4096, rank 32: 17 us (16 MB of x, 1.0 TB/s; the adapters come from L2 once for every 16 tokens).
 
 template <int NT>
 __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width,

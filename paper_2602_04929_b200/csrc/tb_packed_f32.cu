@@ -3,14 +3,14 @@
 //
 // A float is the sum of three bf16 pieces (all 24 bits), and c - z is exact in bf16, so three products with float sums lose nothing
 // that one in float would keep.  The scale is a row's and a run's of columns.  Forward, the contraction runs along the row: the sum of
-// a step is scaled.  Backward it runs down the rows, so dy takes the scale before it is split, which needs a tile
-// whose columns have one group: 32 columns (COLS) where groups are not multiples of 128.
+// a step is scaled.  Backward it runs down the rows, so dy takes the scale before it is split, which needs a tile whose columns have
+// one group: 32 columns (COLS) where groups are not multiples of 128.
 //
-// A step takes 32 of the contraction and its sum joins a float sum: the matrix instruction drops bits of its sum instead of rounding, so
-// long sums in it are off by 2^-24 of their size a step, all to one side.  Activations are split and codes decoded once for the CTA, into shared memory (two buffers; rows
-// padded so that ldmatrix meets no bank twice), while the step before is multiplied; the next step's words are on their way in
-// registers.  A cluster (cs CTAs) shares the contraction where tiles are few, and its sums are joined in a fixed order.  Adapters join
-// the finished sums on the FP32 pipe.
+// A step takes 32 of the contraction and its sum joins a float sum: the matrix instruction drops bits of its sum instead of rounding,
+// so long sums in it are off by 2^-24 of their size a step, all to one side.  Activations are split and codes decoded once for the CTA,
+// into shared memory (two buffers; rows padded so that ldmatrix meets no bank twice), while the step before is multiplied; the next
+// step's words are on their way in registers.  A cluster (cs CTAs) shares the contraction where tiles are few, and its sums are joined
+// in a fixed order.  Adapters join the finished sums on the FP32 pipe.
 //
 // 1024 tokens x 8192 x 8192, 4 bits: 2128 us forward, 194 TFLOP/s of bf16 products (a library's float product of that shape, without
 // the dequantizing, takes 2.2 ms); 4096 x 4096, 603 us.  It is bound by the load/store unit: fragments, split activations and codes

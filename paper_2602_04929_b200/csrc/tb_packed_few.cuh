@@ -1,14 +1,13 @@
-// y = x Q^T for a few tokens (up to 32 in bf16, 96 in float): mma.sync on weights decoded in registers.
+// y = x Q^T where tokens are few or the work is small: mma.sync on weights decoded in registers.
 //
-// With few tokens the product is bound by reading the packed words and, at two to four bits, as much by the instructions that
-// decode them (logical operations go at half rate), so the words are
-// decoded straight into fragments.  A weight row is a
-// row of operand A (16 rows a tile, MT tiles a CTA), tokens are operand B's columns (NT tiles of 8).  Which contraction columns a
-// fragment calls k = 0 .. 15 does not matter as long as both operands agree: a lane takes 32 neighbouring codes of a row (BITS
-// words), hence its quad 128 columns, and the same columns of x; 16 codes decode to the eight registers that four MMAs take.  With
-// two and four bits a pair of neighbours in a register is a code of a word's lower half and the one 16 bits above it, so that a
-// mask extracts both, and it is x that is brought into that order, once for all MT tiles.  c - z is exact in bf16; the scale of a
-// row and of the 128 columns multiplies the sum.  Float activations go through three bf16 pieces, all 24 bits.
+// With few tokens the product is bound by reading the packed words and, at two to four bits, as much by the instructions that decode
+// them (logical operations go at half rate), so the words are decoded straight into fragments.  A weight row is a row of operand A (16
+// rows a tile, MT tiles a CTA), tokens are operand B's columns (NT tiles of 8).  Which contraction columns a fragment calls k = 0 .. 15
+// does not matter as long as both operands agree: a lane takes 32 neighbouring codes of a row (BITS words), hence its quad 128 columns,
+// and the same columns of x; 16 codes decode to the eight registers that four MMAs take.  With two and four bits a pair of neighbours
+// in a register is a code of a word's lower half and the one 16 bits above it, so that a mask extracts both, and it is x that is
+// brought into that order, once for all MT tiles.  c - z is exact in bf16; the scale of a row and of the 128 columns multiplies the
+// sum.  Float activations go through three bf16 pieces, all 24 bits.
 //
 // The words come by TMA, in stages of eight blocks of 128 columns (one for every warp), as many stages ahead as fit beside a second
 // CTA: a warp that loads its own words has too few bytes in flight for the memory's latency.  A tile has the most rows (16 MT) that
