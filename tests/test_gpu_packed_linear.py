@@ -668,3 +668,41 @@ def test_inputs_and_scratch_that_end_with_their_memory(n_tok, rows, d, bits, gro
         pu.near(dx, ref["dx"][0], ref["dx"][1], "dx")
         pu.near(dB, ref["dB"][0], ref["dB"][1], "dB")
     assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("n_tok,rows,d,rank,n_req,dtype", [(70, 4104, 1024, 64, 40, BF), (400, 1032, 768, 32, 3, BF), (2300, 264, 1056, 128, 4, BF), (130, 264, 512, 16, 5, F32)])
+def test_tiles_captured_and_between_guards(n_tok, rows, d, rank, n_req, dtype):
+    """The paths of many tokens in a graph, replayed with other inputs beside eager calls; outputs in the middle of guard values."""
+    tb = _tb()
+    cuts = torch.sort(torch.randint(0, n_tok + 1, (n_req - 1,), generator=torch.Generator().manual_seed(n_tok))).values.tolist()
+    ids = torch.randint(-1, 3, (n_req,), generator=torch.Generator().manual_seed(rows)).tolist()
+    p = pu.problem(n_tok, n_tok, rows, d, 4, 32, dtype, 3, rank, [0, *cuts, n_tok], ids)
+    w, a = pu.on_gpu(tb, p)
+    x, dy = p["x"].cuda(), p["dy"].cuda()
+    buf = torch.full((n_tok * rows + 256,), 7.0, dtype=dtype, device="cuda")
+    low = torch.full((n_tok * rank + 256,), 7.0, device="cuda")
+    y, xa = buf[128:128 + n_tok * rows].view(n_tok, rows), low[128:128 + n_tok * rank].view(n_tok, rank)
+
+    def call(**to):
+        out, kept = tb.tb_packed_linear(w, x, a, **to)
+        return (out, kept, *tb.tb_packed_linear_backward(w, dy, a, x=x, xa=kept))
+
+    first = [v.clone() for v in call()]
+    call(y=y, xa=xa)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = call(y=y, xa=xa)
+    for k in range(4):
+        x.mul_(-2.0), dy.mul_(0.5)
+        want = [v.clone() for v in call()]
+        for v in outs:
+            v.zero_()
+        g.replay()
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(outs, want)), k
+    assert not torch.equal(outs[0], first[0])
+    for b in (buf, low):
+        assert (b[:128] == 7).all() and (b[-128:] == 7).all()
+    assert tb.tb_device_error_flag() == 0
