@@ -358,7 +358,8 @@ tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapter
  * dA and dB come together or are both NULL; they are overwritten (zeros for an adapter
  * that no token has), the same bits on every call.  The input comes as x, in full, or
  * as x_codes and x_scales from tb_checkpoint_pack; xa is the forward pass's.  x, codes
- * and xa may be NULL without dA.  dy [n_tok][d_out] of x_type.
+ * and xa may be NULL without dA.  dy [n_tok][d_out] of x_type.  n_tok may be 0, with any
+ * array of tokens NULL, dx among them.
  * In bf16 the weights enter dx rounded to bf16. */
 size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
                                            tb_dtype x_type, long long n_tok);

@@ -169,7 +169,7 @@ extern "C" tb_status tb_packed_linear_backward(const tb_packed_weight* w, const 
   PackedW pw;
   Adapt ad;
   TB_TRY(checked(w, adapters, x_type, n_tok, true, &pw, &ad));
-  if ((dA == nullptr) != (dB == nullptr) || (dA && !ad.n) || (!dx && !dA)) return TB_ERR_INVALID_ARG;
+  if ((dA == nullptr) != (dB == nullptr) || (dA && !ad.n) || (!dx && !dA && n_tok > 0)) return TB_ERR_INVALID_ARG;
   if (!aligned(dA, 16) || !aligned(dB, 16)) return TB_ERR_INVALID_ARG;
   cudaStream_t st = as_stream(stream);
   if (n_tok == 0) {
