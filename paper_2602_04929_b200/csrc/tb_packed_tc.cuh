@@ -604,11 +604,11 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           if (p.part) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (16 * ch + i < n) fo[(16 * ch + i) * p.n_cols] = __uint_as_float(r[i]);
+              if (16 * ch + i < n) fo[(long long)(16 * ch + i) * p.n_cols] = __uint_as_float(r[i]);
           } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (16 * ch + i < n) bo[(16 * ch + i) * p.n_cols] = __float2bfloat16(__uint_as_float(r[i]));
+              if (16 * ch + i < n) bo[(long long)(16 * ch + i) * p.n_cols] = __float2bfloat16(__uint_as_float(r[i]));
           }
         }
         acc_read();
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           if (!lora) k = parts.end, parts.next();
         }
         if (!ok) break;
-        if (store) {
+        if (store) {  // (32 bits hold 127 rows of the 2^24 columns that a call may have)
           if (p.part) {
 #pragma unroll
             for (int i = 0; i < 128; ++i)
