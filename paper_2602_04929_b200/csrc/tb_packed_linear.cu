@@ -106,7 +106,7 @@ static Scratch carve(const PackedW& w, const Adapt& ad, tb_dtype type, long long
   if (type == TB_BF16 && !takes_few(w, ad, type, n_tok, back)) {
     PackedTc p;
     const int cols = back ? w.d_in : w.d_out;
-    n = packed_tc_carve(packed_tc_plan(ad, (int)n_tok, cols, back ? w.d_out : w.d_in), w, ad, (int)n_tok, cols, back, nullptr, &p);
+    n = packed_tc_carve(packed_tc_plan(ad, (int)n_tok, cols, back ? w.d_out : w.d_in, back), w, ad, (int)n_tok, cols, back, nullptr, &p);
   }
   s.product = b.take<char>(n);
   s.bytes = (back && ad.n) || n ? b.total() : 0;

@@ -120,11 +120,11 @@ __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* 
 }
 
 // Tile and splits by an estimate of the clocks, fitted to sweeps of both (64 to 1999 tokens, widths of 1024 to 8192): a stage of 64
-// columns costs its decoding, whatever the tile, and a little for every token, a tile 1500 clocks and what its results take, and
+// columns (backward there are two, one a piece of the weights) costs its decoding, whatever the tile, and a little for every token, a tile 1500 clocks and what its results take, and
 // splits cost writing and adding their float sums.  The adapters' share is further stages of the tile, four slots each (see the
 // kernel), or joins the float sums: 64 tokens of 32 requests, rank 64, 8192 x 512, has 64 such stages and takes 70 us with them, 26 us
 // joined.
-TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum) {
+TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum, bool back) {
   TcPlan best = {};
   double best_cost = 0.0;
   int sms = sm_count();
@@ -140,7 +140,7 @@ TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum) {
       if (tiles > 0x3fffffff) continue;
       const double waves = (double)((tiles + pairs - 1) / pairs);
       const double stage = 600.0 + 0.4 * n_tile;
-      const double plain = waves * (len / 64 * stage + 1500.0 + 6.0 * n_tile);
+      const double plain = waves * (len / 64 * (back ? 2.0 : 1.0) * stage + 1500.0 + 6.0 * n_tile);
       for (int joined = splits > 1; joined <= (splits > 1 || ad.n); ++joined) {
         double cost = plain;
         if (joined) {
@@ -195,7 +195,7 @@ tb_status packed_product_tc(const PackedW& w, const Adapt& ad, const __nv_bfloat
                             float* low, bool back, void* ws, cudaStream_t st) {
   PackedTc p = {};
   p.n_cols = back ? w.d_in : w.d_out, p.n_sum = back ? w.d_out : w.d_in, p.n_tok = (int)n_tok;
-  const TcPlan t = packed_tc_plan(ad, p.n_tok, p.n_cols, p.n_sum);
+  const TcPlan t = packed_tc_plan(ad, p.n_tok, p.n_cols, p.n_sum, back);
   packed_tc_carve(t, w, ad, p.n_tok, p.n_cols, back, static_cast<char*>(ws), &p);
   p.w = w, p.ad = ad, p.low = low, p.out = out;
   p.M = static_cast<const __nv_bfloat16*>(back ? ad.A : ad.B);

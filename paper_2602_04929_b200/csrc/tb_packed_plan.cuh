@@ -35,7 +35,7 @@ struct TcPlan {
   int n_tile, m_tiles, t_tiles, splits, split_len, pairs;
   bool joined;  // float sums, added with the adapters' share by a kernel of their own: with splits, or where runs are many
 };
-TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum);
+TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum, bool back);
 // Scratch of a product from `ws` on (nullptr: only its size).
 size_t packed_tc_carve(const TcPlan& t, const PackedW& w, const Adapt& ad, int n_tok, int n_cols, bool back, char* ws, PackedTc* p);
 // out = in Q^T or in Q, with the adapters' share; makes their low [n_tok][rank] = in M_i^T too.

@@ -10,8 +10,10 @@
 // Scales.  Forward, a scale belongs to a row of the tile and a group of contraction columns, so it leaves the sum: the tile
 // holds c - z, which bf16 has exactly, and the accumulator of a group (at most 2048 columns of it) is taken from one of two TMEM
 // buffers, scaled and added to float registers by the epilogue warps while the other buffer fills.  The product so has no rounding
-// but that of float sums.  Backward, a scale belongs to the contraction row: the weight s (c - z) is rounded to bf16 when it is
-// decoded, which costs more instructions, and the sum stays in tensor memory to its end, one buffer a tile.
+// but that of float sums.  Backward, a scale belongs to the contraction row, so the weight s (c - z) itself is decoded, as two pieces
+// of bf16 (scale8: 2^-16 of the weight in the mean, 2^-13 at most; a single piece would put as large an error on dx as its own rounding
+// does).  Each piece is a stage of its own with the same tokens, twice the products of a single one, and the sum stays in tensor memory
+// to its end, one buffer a tile.
 //
 // Adapters.  scale v M, v [tokens][rank] float, joins the sum as further contraction steps: slots of 16 for a run of tokens with one
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
@@ -26,9 +28,9 @@
 // between the MMAs, on a scheduler shared with busy warps, are what limits it.
 //
 // 4096 tokens x 8192 x 8192, 2 bits: 430-440 us, 1.25-1.28 PFLOP/s (a library's bf16 product settles at 1.37 under the power cap);
-// gradient, 4099 tokens, 419 us, 1.31 PFLOP/s; 8192 tokens x 4096 x 4096, 4 bits, gradient 200 us, 1.38 PFLOP/s.  Bound by the MMA
-// warp's share of its scheduler and, in long runs, by the power cap.  Small work is bound by latency: 64 tokens x 4096 x 4096 takes
-// 13 us, 3 of them the start, 3 until the first words are decoded.
+// gradient, two products: 4099 tokens, 860-925 us, 1.28-1.19 PFLOP/s, where a single piece of the weights takes 390; 8192 tokens x 4096 x
+// 4096, 4 bits, 426 us, 1.29 PFLOP/s (204).  Bound by the MMA warp's share of its scheduler and, in long runs, by the power cap.  Small work
+// is bound by latency: 64 tokens x 4096 x 4096 takes 13 us, 3 of them the start, 3 until the first words are decoded.
 #pragma once
 
 #include "tb_packed.cuh"
@@ -71,11 +73,24 @@ struct Parts {
   }
 };
 
-// c - z, exact, times s, rounded to bf16: s as two bf16 pieces, the smaller product rounded first, 2^-8 of the last place of the
-// result; the fused multiply-add rounds the sum
-__device__ __forceinline__ void scale8(unsigned (&o)[4], unsigned hi, unsigned lo) {
+// c - z, exact, times s, as two pieces of bf16; s comes in two as well, hi and lo.  The first piece is (c - z) s less about 2^-7 of it,
+// rounded; the second is what that leaves, 2^-9.5 to 2^-6.1 of the weight, so that both have the weight's sign and an infinite dy
+// comes to the infinity that it should (a remainder of either sign would give infinity less infinity).  (c - z) hi less the first piece is
+// exact for codes of four bits, else rounded like the second piece itself: at most 2^-14.1 of the weight each.
+struct ScalePieces {
+  unsigned hi, lo, less;  // twice each
+  __device__ __forceinline__ void set(unsigned v) {
+    hi = __byte_perm(v, 0, 0x3232), lo = __byte_perm(v, 0, 0x1010);
+    less = bf2(__hmul2(bf2(hi), __float2bfloat162_rn(0.9921875f)));
+  }
+};
+template <int PIECE>
+__device__ __forceinline__ void scale8(unsigned (&o)[4], const ScalePieces& s) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = bf2(__hfma2(bf2(o[i]), bf2(hi), __hmul2(bf2(o[i]), bf2(lo))));
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 q = bf2(o[i]), first = __hfma2(q, bf2(s.less), __hmul2(q, bf2(s.lo)));
+    o[i] = bf2(PIECE == 0 ? first : __hfma2(q, bf2(s.lo), __hfma2(q, bf2(s.hi), __hneg2(first))));
+  }
 }
 
 __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
@@ -83,7 +98,7 @@ __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
 }
 
 // The packed words on their way to the decode warps: 128 columns of the CTA's 128 weight rows (forward, two stages) or of 64 weight
-// rows (backward, one stage), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points,
+// rows (backward, two stages, one a piece), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points,
 // backward each beside its scale.  A ring of STAGES such units.  Rows of 32, 64 and 128 bytes are swizzled, so that neighbouring threads' rows lie
 // in different banks.
 template <int BITS, bool BACK>
@@ -96,13 +111,13 @@ struct Raw {
     PAD = (BYTES + 1023) & ~1023,  // swizzled rows start on a multiple of their pattern
     MMA_STAGES = BITS <= 4 ? 6 : 4,  // even: the MMA warp takes two at a time
     ROOM = PT_SMEM - 1024 - 512 - MMA_STAGES * PT_STAGE_BYTES,
-    TURNS = BACK ? 4 : 2,  // decode warpgroups, which take the units in turn
     FIT = ROOM / PAD < 8 ? ROOM / PAD : 8,
-    // a whole number of turns, so that a slot is always the same warpgroup's: waits go by parity, and one that skipped a phase of
-    // the barrier that it looks at would take the phase before for its own
-    STAGES = FIT / TURNS * TURNS
+    // units go to a warpgroup in turn with another (backward: to two of them, one a piece, in turn with the other two).  A whole number
+    // of turns, so that a slot is always the same ones': waits go by parity, and one that skipped a phase of the barrier that it looks
+    // at would take the phase before for its own
+    STAGES = FIT / 2 * 2
   };
-  static_assert(STAGES >= TURNS, "the ring holds a unit for every warpgroup");
+  static_assert(STAGES >= 2, "the ring holds a unit for every turn");
   // 16-byte piece c of row r
   static __device__ __forceinline__ uint32_t piece(int r, int c) {
     if constexpr (ROW == 32) return r * ROW + ((c ^ ((r >> 2) & 1)) << 4);
@@ -117,15 +132,17 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-template <int BITS, int C, bool BACK>
-__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const unsigned (&s)[2][2], uint32_t row_addr,
+// 64 neighbouring codes of a row into the tile: c - z, or (PIECE) a piece of s (c - z).
+enum { PLAIN = -1 };
+template <int BITS, int C, int PIECE>
+__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
                                            uint32_t sw) {
   if constexpr (C < 8) {
     unsigned o[4];
     decode8<BITS, 8 * C>(w, z[C / 4], o);
-    if constexpr (BACK) scale8(o, s[C / 4][0], s[C / 4][1]);
+    if constexpr (PIECE != PLAIN) scale8<PIECE>(o, s[C / 4]);
     sts16(row_addr + ((C ^ sw) << 4), o);
-    decode_row<BITS, C + 1, BACK>(w, z, s, row_addr, sw);
+    decode_row<BITS, C + 1, PIECE>(w, z, s, row_addr, sw);
   }
 }
 
@@ -144,7 +161,7 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
 
 template <bool BACK>
 struct Roles {
-  enum { DECODE = Raw<2, BACK>::TURNS, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
+  enum { DECODE = BACK ? 4 : 2, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
 };
 
 template <int BITS, bool BACK>
@@ -185,7 +202,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     }
     for (int s = 0; s < 8; ++s) {
       mbar_init(raw_full(s), 1);
-      mbar_init(raw_empty(s), 4);
+      mbar_init(raw_empty(s), BACK ? 8 : 4);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf_bar(b), 1);
@@ -229,6 +246,8 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     r.lora = ((r.n_runs * nb * 2 + 7) >> 3) * 2;  // stages of four slots, an even number of them
     return r;
   };
+  // stages of a tile's product; backward two for every 64 rows of the contraction, so always an even number
+  auto stages_of = [&](const Tile& c) { return (c.k1 - c.k0 + PT_BK - 1) / PT_BK * (BACK ? 2 : 1); };
 
   if (warp < 4) {
     if (!BACK) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -238,7 +257,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       bool ok = true;
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
-        const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
+        const int n_st = stages_of(c);
         for (int st = 0; st < n_st + c.lora; ++st, ++it) {
           const int s = it % STAGES;
           if (!mbar_wait(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error)) {
@@ -250,7 +269,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               mbar_expect_tx(full_bar(s), 2u * half_n * PT_BK * 2u);
             else
               mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
-            tma_load_2d_pair(base + s * PT_STAGE_BYTES + PT_A_BYTES, &xmap, c.k0 + st * PT_BK, c.t0 + (int)rank * half_n,
+            tma_load_2d_pair(base + s * PT_STAGE_BYTES + PT_A_BYTES, &xmap, c.k0 + (BACK ? st >> 1 : st) * PT_BK, c.t0 + (int)rank * half_n,
                              map_to_rank(full_bar(s), 0));
           } else {
             mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
@@ -283,12 +302,13 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       };
       for (int t = pair; t < n_tiles && ok; t += n_pairs) {
         const Tile c = tile_of(t);
-        const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
+        const int n_st = stages_of(c);
         int st = 0, left = 0;
-        // accumulations of one length and of whole pairs of stages: nothing to keep but how many pairs are left
-        const int len = BACK ? c.k1 - c.k0 : parts.part;
-        const bool regular = BACK || (group % len == 0 && c.k0 % len == 0 && c.k1 % len == 0);
-        if (regular && len % (2 * PT_BK) == 0 && s % 2 == 0) {
+        // accumulations of one length and of whole pairs of stages: nothing to keep but how many pairs are left.  Backward all are: an
+        // accumulation is the tile's, a pair is two pieces, and what lies behind the last row is zeros
+        const int len = BACK ? n_st * PT_BK : parts.part;
+        const bool regular = BACK || (group % len == 0 && c.k0 % len == 0 && c.k1 % len == 0 && len % (2 * PT_BK) == 0 && s % 2 == 0);
+        if (regular) {
           uint32_t d = 0, more = 0;
           for (; st < n_st; st += 2) {
             if (left == 0) {
@@ -330,7 +350,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = s * (PT_STAGE_BYTES >> 4);
           const uint64_t bd = b_main + at;
-          if (st < n_st) {
+          if (!BACK && st < n_st) {
             const uint64_t ad = a_main + at;
             const int steps = min(4, todo);
             todo -= steps;
@@ -339,18 +359,18 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               if (left == 0) {
                 ok = acc_free();
                 if (!ok) break;
-                left = BACK ? todo + steps - kk : (min(parts.end, c.k1) - k + 15) >> 4;
+                left = (min(parts.end, c.k1) - k + 15) >> 4;
                 parts.next();
                 more = 0;
               }
               --left;
               if (one) {
                 umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, ad + kk * a_step, bd + kk * b_step, id_main, more);
-                if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
+                if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
               }
               __syncwarp();
               k += 16;
-              if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
+              if (left == 0) ++acc_it;
             }
             if (!ok) break;
             if (one) umma_commit_pair(empty_bar(s));
@@ -426,12 +446,13 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     const uint32_t row_off = BACK ? (uint32_t)(tid >> 6) * 8192u + (uint32_t)my_row * 128u : (uint32_t)my_row * 128u;
     const uint32_t sw = (uint32_t)(my_row & 7);
     const bool one_sz = p.w.group % 128 == 0;
-    constexpr int PER = BACK ? 1 : 2;  // stages of a unit
+    // forward, a unit is two stages of a warpgroup; backward it is one of each of two, and `unit` counts stages: odd ones are second pieces
+    constexpr int PER = BACK ? 1 : 2;
     uint32_t it = 0, unit = 0, tiles = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile c = tile_of(t);
-      const int n_st = (c.k1 - c.k0 + PT_BK - 1) / PT_BK;
+      const int n_st = stages_of(c);
       if (p.n_runs && tiles > 0) {
         ok = mbar_wait_warp(tile_bar, (tiles - 1) & 1u, abort_flag, &g_packed_error);
         if (!ok) break;
@@ -443,8 +464,8 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           it += here;
           continue;
         }
-        const uint32_t rs = unit % Ring::STAGES;
-        ok = mbar_wait_warp(raw_full(rs), (unit / Ring::STAGES) & 1u, abort_flag, &g_packed_error);
+        const uint32_t in_ring = BACK ? unit >> 1 : unit, rs = in_ring % Ring::STAGES;
+        ok = mbar_wait_warp(raw_full(rs), (in_ring / Ring::STAGES) & 1u, abort_flag, &g_packed_error);
         if (!ok) break;
         const unsigned char* q = gen_base + (raw_base - base) + rs * Ring::PAD;
 #pragma unroll
@@ -453,7 +474,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           // outside the matrix the words are zeros and any zero-point gives finite values, which meet zeros or are not stored
           const int half = BACK ? tid >> 6 : i;  // of the unit's 128 columns
           unsigned w[2 * BITS], z[2];
-          unsigned sc[2][2] = {};
+          ScalePieces sc[2];
           if constexpr (BITS % 2 == 0) {
 #pragma unroll
             for (int e = 0; e < BITS / 2; ++e) {
@@ -473,7 +494,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             if constexpr (BACK) {
               const uint2 v = reinterpret_cast<const uint2*>(q + Ring::Z)[o];
               z[h] = v.x;
-              sc[h][0] = __byte_perm(v.y, 0, 0x3232), sc[h][1] = __byte_perm(v.y, 0, 0x1010);
+              sc[h].set(v.y);
             } else {
               z[h] = reinterpret_cast<const unsigned*>(q + Ring::Z)[o];
             }
@@ -485,7 +506,13 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           const int s = it % STAGES;
           ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
           if (!ok) break;
-          decode_row<BITS, 0, BACK>(w, z, sc, base + s * PT_STAGE_BYTES + row_off, sw);
+          const uint32_t to = base + s * PT_STAGE_BYTES + row_off;
+          if constexpr (!BACK)
+            decode_row<BITS, 0, PLAIN>(w, z, sc, to, sw);
+          else if (turn & 1)
+            decode_row<BITS, 0, 1>(w, z, sc, to, sw);
+          else
+            decode_row<BITS, 0, 0>(w, z, sc, to, sw);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));

@@ -66,3 +66,41 @@ def test_the_widest_rows(dtype):
     y, _ = tb.tb_packed_linear(w, x)
     assert tb.tb_device_error_flag() == 0
     check(y, x, Q.T)
+
+
+@pytest.mark.parametrize("rows,d,bits,group,n_tok", [(1032, 544, 4, 32, 70), (2056, 1024, 2, 128, 300), (4104, 256, 8, 0, 40), (520, 1152, 7, 384, 700), (8, 160, 3, 32, 5),
+                                                     (72, 160, 5, 32, 33), (200, 128, 6, 0, 1100)])
+def test_input_gradient_with_all_of_the_weights(rows, d, bits, group, n_tok):
+    """dx is off by float sums, by 2^-13 of every weight at most (a second bf16 piece of up to 2^-6.1 of it, off by 2^-8 of itself, twice where
+    codes have more than four bits) and by its own rounding.  That rounding alone is 1.66e-3 in the norm (2^-8 / sqrt 3 at the power of two,
+    times the mean of 1 / m^2 over mantissas m, whose root is 0.74); weights rounded to bf16 would add as much again."""
+    tb = _tb()
+    p = pu.problem(rows, n_tok, rows, d, bits, group, BF)
+    w, _ = pu.on_gpu(tb, p)
+    dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    dy, Q = p["dy"].double(), p["Q"]
+    want, size = dy @ Q, dy.abs() @ Q.abs()
+    weights = ((rows + 64) * 2.0 ** -23 + 2.0 ** (-14 if bits <= 4 else -13)) * size
+    pu.near(dx, want, weights + pu.HALF_STEP[BF] * (want.abs() + weights), "dx")
+    if dx.numel() > 10000:
+        assert pu.norm_off(dx, want) <= 2.0 ** -9
+    assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("bits,group", [(2, 128), (4, 32), (7, 0)])
+@pytest.mark.parametrize("n_tok", [3, 300])
+def test_an_infinite_gradient_meets_the_weights(bits, group, n_tok):
+    """dy of infinity gives what the formula says, both pieces of a weight having its sign: an infinity of the weight's sign, and what is no
+    number where the weight is 0."""
+    tb = _tb()
+    p = pu.problem(bits, n_tok, 136, 256, bits, group, BF)
+    clean = p["dy"].clone()
+    p["dy"][0, 30], p["dy"][1, 135], p["dy"][2, 7] = float("inf"), float("-inf"), float("nan")
+    w, _ = pu.on_gpu(tb, p)
+    dx = tb.tb_packed_linear_backward(w, p["dy"].cuda())[0].cpu().double()
+    for t, j in ((0, 30), (1, 135)):
+        k = p["Q"][j]
+        assert torch.isnan(dx[t][k == 0]).all() and torch.equal(dx[t][k != 0], p["dy"][t, j].double() * k[k != 0])
+    assert torch.isnan(dx[2]).all()
+    want, bound = pu.backward64(dict(p, dy=clean))["dx"]
+    pu.near(dx[3:], want[3:], bound[3:], "dx") if n_tok > 3 else None
