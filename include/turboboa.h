@@ -341,8 +341,11 @@ typedef struct {
  *   x  [n_tok][d_in], y [n_tok][d_out]: bf16 or float (x_type), 16-byte aligned
  *   xa [n_tok][rank] float, required with adapters: x_t A_i^T of every token, not
  *      scaled, zero for a token without an adapter; the backward pass takes it
- * Sums are float and are rounded to the type of y once.  A value that is not finite
- * reaches the outputs of its own token alone, and one in an adapter those of its requests.
+ * Sums are float and are rounded to the type of y once.  Products x (c - z) are summed
+ * over the columns of a scale (or some of them) before the scale multiplies: where that
+ * sum passes the largest float, y is infinite or no number, whatever the scale.
+ * A value that is not finite reaches the outputs of its own token alone, and one in an
+ * adapter those of its requests.
  * n_tok may be 0.  Workspace: tb_packed_linear_workspace bytes (may be 0). */
 size_t tb_packed_linear_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
                                   tb_dtype x_type, long long n_tok);

@@ -430,10 +430,6 @@ __device__ __forceinline__ unsigned pair_bf16(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const unsigned*>(&v);
 }
-__device__ __forceinline__ float rest_of(float v, unsigned bits) {  // of v without its bf16 piece; nothing of what is not finite
-  const float f = __uint_as_float(bits);
-  return fabsf(f) <= 3.3895e38f ? v - f : 0.0f;
-}
 
 template <int RP, bool EIGHT>
 __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
@@ -539,7 +535,7 @@ __global__ void __launch_bounds__(AG_THREADS, RP == 128 ? 1 : 2)
       if (EIGHT) v[0] *= fv[k], v[1] *= fv[k], v[2] *= fv[k], v[3] *= fv[k];
 #pragma unroll
       for (int p = 0; p < 3; ++p) {
-        const unsigned a = pair_bf16(v[0], v[1]), b = pair_bf16(v[2], v[3]);
+        const unsigned a = first_pieces(v[0], v[1]), b = first_pieces(v[2], v[3]);
         const int n = p * RP + r;
         sts8(stage + S::A_BYTES + (n >> 6) * 8192 + lt * 128 + ((((n & 63) >> 3) ^ (lt & 7)) << 4) + (n & 7) * 2, a, b);
         if (p < 2) {

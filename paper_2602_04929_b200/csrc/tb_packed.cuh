@@ -38,6 +38,18 @@ __device__ __forceinline__ int adapter_of(const Adapt& a, long long t) {
 // The input of a product of gradients: in full, or 8-bit codes with a scale for a token and CKPT_RUN columns.
 constexpr int CKPT_RUN = 128;
 
+// Pieces of floats: two floats truncated to bf16, and what that leaves of one of them, nothing of what is not finite.  A piece takes
+// eight bits, so that three hold a float; rounded to the nearest, the first piece of a value above 3.396e38 would be infinite.
+__device__ __forceinline__ unsigned first_pieces(float lo, float hi) {
+  unsigned o;
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
+  return o;
+}
+__device__ __forceinline__ float rest_of(float v, unsigned piece) {  // `piece` in the upper half, as a float's bits
+  const float f = __uint_as_float(piece);
+  return fabsf(f) < __int_as_float(0x7f800000) ? v - f : 0.0f;
+}
+
 int sm_count();  // of the current device, 0 where it cannot be asked
 
 }  // namespace tb

@@ -60,12 +60,8 @@ __device__ __forceinline__ void load_acts(const float* p, Acts<3>& a) {
   for (int n = 0; n < 3; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-      a.v[n][i] = bf2(b);
-      // what is left, nothing of what is not finite (or rounds to infinity)
-      const float lo = __uint_as_float(a.v[n][i] << 16), hi = __uint_as_float(a.v[n][i] & 0xffff0000u);
-      f[2 * i] = fabsf(lo) <= 3.3895e38f ? f[2 * i] - lo : 0.0f;
-      f[2 * i + 1] = fabsf(hi) <= 3.3895e38f ? f[2 * i + 1] - hi : 0.0f;
+      a.v[n][i] = first_pieces(f[2 * i], f[2 * i + 1]);
+      f[2 * i] = rest_of(f[2 * i], a.v[n][i] << 16), f[2 * i + 1] = rest_of(f[2 * i + 1], a.v[n][i] & 0xffff0000u);
     }
 }
 
@@ -129,10 +125,8 @@ __device__ __forceinline__ void pieces16(const Raw16<3>& x, Acts16<3>& a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float &fl = f[Pair<BITS>::lo(i)], &fh = f[Pair<BITS>::hi(i)];
-      a.v[n][i] = bf2(__floats2bfloat162_rn(fl, fh));
-      const float lo = __uint_as_float(a.v[n][i] << 16), hi = __uint_as_float(a.v[n][i] & 0xffff0000u);
-      fl = fabsf(lo) <= 3.3895e38f ? fl - lo : 0.0f;
-      fh = fabsf(hi) <= 3.3895e38f ? fh - hi : 0.0f;
+      a.v[n][i] = first_pieces(fl, fh);
+      fl = rest_of(fl, a.v[n][i] << 16), fh = rest_of(fh, a.v[n][i] & 0xffff0000u);
     }
 }
 

@@ -150,12 +150,13 @@ __device__ __forceinline__ bool not_finite2(unsigned v) {
   return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
 }
 
-// bf16 pieces of v: the value rounded, and what that leaves rounded (nothing where the value is not finite or rounds to infinity)
+// bf16 pieces of v: the value rounded (a finite one to no more than the largest of bf16), and what that leaves rounded, nothing of what
+// is not finite
 __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
-  const __nv_bfloat16 hi = __float2bfloat16(v);
+  constexpr float top = 3.38953139e38f;  // (2 - 2^-7) 2^127
+  const __nv_bfloat16 hi = __float2bfloat16(fabsf(v) <= 3.40282347e38f ? fminf(fmaxf(v, -top), top) : v);
   if (piece == 0) return *reinterpret_cast<const unsigned short*>(&hi);
-  const float h = __bfloat162float(hi);
-  const __nv_bfloat16 lo = __float2bfloat16(fabsf(h) <= 3.3895e38f ? v - h : 0.0f);
+  const __nv_bfloat16 lo = __float2bfloat16(rest_of(v, __float_as_uint(__bfloat162float(hi))));
   return *reinterpret_cast<const unsigned short*>(&lo);
 }
 

@@ -68,6 +68,61 @@ def test_the_widest_rows(dtype):
     check(y, x, Q.T)
 
 
+def _within_one(p):
+    """The problem with codes of two bits and zero-points of 1 whose differences are -1, 0 and 1."""
+    codes = np.random.default_rng(6).integers(0, 3, (p["rows"], p["d"]))
+    p["packed"], p["zeros"] = torch.from_numpy(pu.pack_rows(codes, 2).copy()), torch.ones_like(p["zeros"])
+    p["Q"] = torch.from_numpy(codes - 1).double() * p["scales"].double().repeat_interleave(p["group"], 1)
+    return p
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("n_tok", [3, 40, 97, 200, 1400])
+def test_the_largest_activations(n_tok, group, dtype):
+    """The largest finite values, where no sum of x (c - z) leaves the range of floats (|c - z| <= 1 here): those of y and dx are finite,
+    and right.  3.3953e38 lies between the largest bf16 and what rounds to infinity."""
+    tb = _tb()
+    p = _within_one(pu.problem(5, n_tok, 264, 256, 2, group, dtype))
+    top = torch.finfo(dtype).max
+    for t, v in ((0, top), (1, -top), (2, 3.3953e38 if dtype == F32 else -top)):
+        p["x"][t, 17 + t], p["dy"][t, 30 + t] = v, v
+    w, _ = pu.on_gpu(tb, p)
+    y, _ = tb.tb_packed_linear(w, p["x"].cuda())
+    want, _, bound = pu.forward64(p)
+    pu.near(y, want, bound, "y")
+    dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda())
+    pu.near(dx, *pu.backward64(p)["dx"], "dx")
+    assert tb.tb_device_error_flag() == 0
+
+
+@pytest.mark.parametrize("dtype,n_tok", [(BF, 600), (F32, 40), (F32, 200)])
+@pytest.mark.parametrize("rank", [8, 40])
+def test_the_largest_sums_of_the_narrow_product(dtype, n_tok, rank):
+    """x A^T next to the largest float (3.3995e38 rounds to infinity in bf16), met by small entries of B and of dy: finite outputs and
+    gradients."""
+    tb = _tb()
+    p = _within_one(pu.problem(3, n_tok, 520, 256, 2, 128, dtype, 1, rank, [0, n_tok], [0]))
+    p["A"].zero_(), p["B"].mul_(1e-3), p["scale"].fill_(1.0)
+    p["A"][0, :, 7:9] = 1.0
+    p["x"][:4] *= 2.0 ** -100
+    p["x"][:4, 7] = torch.tensor([3.0e38, 3.3895314e38, -3.3895314e38, 3.3895314e38]).to(dtype)
+    p["x"][3, 8] = 1e36
+    p["scales"], p["Q"] = p["scales"] * 2.0 ** -20, p["Q"] * 2.0 ** -20       # the product itself stays far below the adapters' share
+    w, a = pu.on_gpu(tb, p)
+    y, xa = tb.tb_packed_linear(w, p["x"].cuda(), a)
+    want, xa64, bound = pu.forward64(p)
+    pu.near(xa[:4], xa64[:4], 2.0 ** -22 * xa64[:4].abs(), "xa")
+    pu.near(y, want, bound, "y")
+    xa = xa.clone()
+    xa[0], xa[2] = 3.3953e38, -3.4028e38
+    p["dy"] = p["dy"] * 2.0 ** -30
+    out = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a, x=p["x"].cuda(), xa=xa)
+    ref = pu.backward64(p, None, xa.cpu())
+    for got, name in zip(out, ("dx", "dA", "dB")):
+        pu.near(got, *ref[name], name)
+
+
 @pytest.mark.parametrize("rows,d,bits,group,n_tok", [(1032, 544, 4, 32, 70), (2056, 1024, 2, 128, 300), (4104, 256, 8, 0, 40), (520, 1152, 7, 384, 700), (8, 160, 3, 32, 5),
                                                      (72, 160, 5, 32, 33), (200, 128, 6, 0, 1100)])
 def test_input_gradient_with_all_of_the_weights(rows, d, bits, group, n_tok):
