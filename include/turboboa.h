@@ -315,10 +315,10 @@ typedef struct {
                                  divides d_in                                       */
   const unsigned int* packed; /* [d_out][d_in * bits / 32], 16-byte aligned         */
   const float* scales;        /* [d_out][n_g]                                       */
-  const int* zeros;           /* [d_out][n_g].  The quantizer's, 0 .. 2^bits - 1, and
-                                 any in -128 .. 128 are exact; where code - zero
-                                 needs more than bf16's eight bits, it is rounded
-                                 to about as many                                   */
+  const int* zeros;           /* [d_out][n_g].  code - zero is exact up to 256, which
+                                 the quantizer's zeros, 0 .. 2^bits - 1, always
+                                 keep; beyond, where it needs more than bf16's eight
+                                 bits, it is off by 2^-6 of itself at most           */
 } tb_packed_weight;
 
 /* Low-rank adapters of the requests in a batch.  Request j has the tokens starts[j] ..

@@ -1,4 +1,4 @@
-// Packed codes to bf16 integers c - z, exact for |c - z| <= 256.
+// Packed codes to bf16 integers c - z, exact for |c - z| <= 256 (with the zero-point's second piece, where it has one).
 #pragma once
 
 #include "tb_common.cuh"
@@ -27,14 +27,25 @@ __device__ __forceinline__ unsigned masked(unsigned v, unsigned mask, unsigned b
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(o) : "r"(v), "r"(mask), "r"(bits));
   return o;
 }
-// small integers to float without the conversion unit
-__device__ __forceinline__ float small_float(int v) { return __int_as_float(0x4B400000 + v) - 12582912.0f; }
-
-// A zero-point as the decoders take it: -(128 + z) twice in bf16, or 2^23 + z in float for eight bits.
+// A zero-point as the decoders take it: 2^23 + z in float for eight bits, else -(128 + z) in two pieces of bf16, the first (in the upper
+// half) truncated: what a code and the first piece come to so is no larger than c - z, and exact where that is.  The second piece is 0 for
+// -384 <= z <= 128, which a zero-point among the codes always is, so it is added where a warp meets one that is not.
 __device__ __forceinline__ unsigned zero_word(int z, int bits) {
-  if (bits == 8) return __float_as_uint((float)(8388608 + z));
-  z = max(-4000000, min(4000000, z));  // far beyond what eight bits keep apart
-  return bf2(__float2bfloat162_rn(-128.0f - small_float(z)));
+  if (bits == 8) return __float_as_uint((float)z + 8388608.0f);
+  const float v = -128.0f - (float)z, first = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  return __byte_perm(bf2(__float2bfloat162_rn(v - first)), __float_as_uint(v), 0x7610);
+}
+template <int BITS>
+__device__ __forceinline__ unsigned zero_first(unsigned word) {  // twice, as decode8 takes it
+  return BITS == 8 ? word : __byte_perm(word, 0, 0x3232);
+}
+template <int BITS>
+__device__ __forceinline__ unsigned zero_second(unsigned word) {  // twice
+  return BITS == 8 ? 0u : __byte_perm(word, 0, 0x1010);
+}
+template <int BITS>
+__device__ __forceinline__ bool has_second(unsigned words) {  // of one word, or of several or-ed together
+  return BITS < 8 && (words & 0xffffu) != 0;
 }
 // Codes C0 .. C0 + 7 of a lane's words as four pairs of bf16 holding c - z.  A code placed in the low mantissa bits of 128.0
 // is 128 + c (up to seven bits), and 128 + z is subtracted; to bring neighbours 16 bits apart, a field of codes (at most 16 bits)

@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(F_THREADS, 2) k_packed_f32(PackedF32 p) {
       if (32 * i < shift + 16 * w.bits) v[i] = r[i];
     if (!BACK && s > s0 && k0 % w.group) return;  // the group's zero-point is at hand
     const int z = w.zeros[(long long)row * w.n_g + (BACK ? group0 : col / w.group)];
-    zero = (float)(8388608 + max(-4000000, min(4000000, z)));
+    zero = (float)z + 8388608.0f;
   };
   auto store = [&](int buffer) {
     char* a = smem + buffer * L::BUFFER;

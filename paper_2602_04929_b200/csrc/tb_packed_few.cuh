@@ -81,6 +81,23 @@ __device__ __forceinline__ void few_step(const unsigned (&w0)[N], const unsigned
     }
 }
 
+// The zero-points' second pieces, the same for every code of a row: as further weights beside the same activations.
+template <int NP>
+__device__ __forceinline__ void few_second(unsigned z0, unsigned z1, const unsigned (&x)[NP][4], float (&acc)[4]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    mma_few(acc, z0, z1, z0, z1, x[p][0], x[p][1]);
+    mma_few(acc, z0, z1, z0, z1, x[p][2], x[p][3]);
+  }
+}
+template <int NP>
+__device__ __forceinline__ void few_second(unsigned z0, unsigned z1, const unsigned (&x)[NP][8], float (&acc)[4]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) mma_few(acc, z0, z1, z0, z1, x[p][i], x[p][i + 1]);
+}
+
 // Columns of register i of 16: the lower half's, the upper half's.
 template <int BITS>
 struct Pair {
@@ -272,15 +289,17 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
       Acts16<NP> a[2][NT];
       unsigned z[2 * MT];
       float sc[2 * MT];
+      unsigned seconds = 0;
       if (mine) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int n = 0; n < NT; ++n) pieces16<BITS>(next.x[h][n], a[h][n]);
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) z[i] = zero_word(next.z[i], BITS), sc[i] = next.s[i];
+        for (int i = 0; i < 2 * MT; ++i) z[i] = zero_word(next.z[i], BITS), seconds |= z[i], sc[i] = next.s[i];
         if (b + 8 < b_end) fetch(b + 8);
       }
+      const bool second = BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(seconds));
       const bool landed = __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * s, phase, &gave_up, &g_few_error));
       if (mine && landed) {  // (a wait that gave up leaves its share out; nobody skips a barrier)
         const unsigned char* stage = ring + s * STAGE;
@@ -291,13 +310,25 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
           load_words<BITS, RC>(stage, 16 * m + g, at, w0);
           load_words<BITS, RC>(stage, 16 * m + 8 + g, at, w1);
           float acc[NT][4] = {};
-          few_step16<BITS, 0, NT, NP>(w0, w1, z[2 * m], z[2 * m + 1], a[0], acc);
-          few_step16<BITS, 1, NT, NP>(w0, w1, z[2 * m], z[2 * m + 1], a[1], acc);
+          const unsigned z0 = zero_first<BITS>(z[2 * m]), z1 = zero_first<BITS>(z[2 * m + 1]);
+          few_step16<BITS, 0, NT, NP>(w0, w1, z0, z1, a[0], acc);
+          few_step16<BITS, 1, NT, NP>(w0, w1, z0, z1, a[1], acc);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[m][n][c] = fmaf(sc[2 * m + (c >> 1)], acc[n][c], sum[m][n][c]);
         }
+        if (second)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float acc[4] = {};
+              few_second<NP>(zero_second<BITS>(z[2 * m]), zero_second<BITS>(z[2 * m + 1]), a[0][n].v, acc);
+              few_second<NP>(zero_second<BITS>(z[2 * m]), zero_second<BITS>(z[2 * m + 1]), a[1][n].v, acc);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) sum[m][n][c] = fmaf(sc[2 * m + (c >> 1)], acc[c], sum[m][n][c]);
+            }
       }
       if (st + p.stages < n_st) {
         __syncthreads();
@@ -331,7 +362,10 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
           z[i] = zero_word(p.w.zeros[sz0 + e * p.w.n_g + gi], BITS);
           s[i] = p.w.scales[sz0 + e * p.w.n_g + gi];
         }
-        few_step<BITS, 0, NT, NP>(w[0], w[1], z[0], z[1], a, acc);
+        few_step<BITS, 0, NT, NP>(w[0], w[1], zero_first<BITS>(z[0]), zero_first<BITS>(z[1]), a, acc);
+        if (BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(z[0] | z[1])))
+#pragma unroll
+          for (int n = 0; n < NT; ++n) few_second<NP>(zero_second<BITS>(z[0]), zero_second<BITS>(z[1]), a[n].v, acc[n]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll

@@ -132,18 +132,29 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// 64 neighbouring codes of a row into the tile: c - z, or (PIECE) a piece of s (c - z).
+// 64 neighbouring codes of a row into the tile: c - z, or (PIECE) a piece of s (c - z).  SECOND: with the zero-points' second pieces.
 enum { PLAIN = -1 };
-template <int BITS, int C, int PIECE>
-__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
-                                           uint32_t sw) {
+template <int BITS, int C, int PIECE, bool SECOND>
+__device__ __forceinline__ void decode_codes(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
+                                             uint32_t sw) {
   if constexpr (C < 8) {
     unsigned o[4];
-    decode8<BITS, 8 * C>(w, z[C / 4], o);
+    decode8<BITS, 8 * C>(w, zero_first<BITS>(z[C / 4]), o);
+    if constexpr (SECOND)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = bf2(__hadd2(bf2(o[i]), bf2(zero_second<BITS>(z[C / 4]))));
     if constexpr (PIECE != PLAIN) scale8<PIECE>(o, s[C / 4]);
     sts16(row_addr + ((C ^ sw) << 4), o);
-    decode_row<BITS, C + 1, PIECE>(w, z, s, row_addr, sw);
+    decode_codes<BITS, C + 1, PIECE, SECOND>(w, z, s, row_addr, sw);
   }
+}
+template <int BITS, int PIECE>
+__device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
+                                           uint32_t sw) {
+  if (BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(z[0] | z[1])))
+    decode_codes<BITS, 0, PIECE, BITS < 8>(w, z, s, row_addr, sw);
+  else
+    decode_codes<BITS, 0, PIECE, false>(w, z, s, row_addr, sw);
 }
 
 __device__ __forceinline__ bool not_finite2(unsigned v) {
@@ -509,11 +520,11 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           if (!ok) break;
           const uint32_t to = base + s * PT_STAGE_BYTES + row_off;
           if constexpr (!BACK)
-            decode_row<BITS, 0, PLAIN>(w, z, sc, to, sw);
+            decode_row<BITS, PLAIN>(w, z, sc, to, sw);
           else if (turn & 1)
-            decode_row<BITS, 0, 1>(w, z, sc, to, sw);
+            decode_row<BITS, 1>(w, z, sc, to, sw);
           else
-            decode_row<BITS, 0, 0>(w, z, sc, to, sw);
+            decode_row<BITS, 0>(w, z, sc, to, sw);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));

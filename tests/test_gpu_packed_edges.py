@@ -123,6 +123,57 @@ def test_the_largest_sums_of_the_narrow_product(dtype, n_tok, rank):
         pu.near(got, *ref[name], name)
 
 
+def _with_zero_points(p, z):
+    d = p["d"]
+    wide = lambda v: v.double().repeat_interleave(d // v.shape[1], 1)  # noqa: E731
+    return dict(p, zeros=z, Q=p["Q"] + wide(p["zeros"].long() - z.long()) * wide(p["scales"]))
+
+
+@pytest.mark.parametrize("bits", range(2, 9))
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n_tok", [5, 24, 97, 1100])
+def test_zero_points_wherever_their_differences_are_exact(bits, dtype, n_tok):
+    """Every zero-point whose differences to all codes lie within 256: the products have nothing but float sums and one rounding, on
+    both sides of every rule that chooses a kernel."""
+    tb = _tb()
+    p = pu.problem(bits, n_tok, 264, 256, bits, 32 if bits % 2 else 128, dtype)
+    g = torch.Generator().manual_seed(bits)
+    z = torch.randint((1 << bits) - 257, 257, p["zeros"].shape, generator=g, dtype=torch.int32)
+    z[::3] = torch.randint(129, 257, z[::3].shape, generator=g, dtype=torch.int32)
+    p = _with_zero_points(p, z)
+    w, _ = pu.on_gpu(tb, p)
+    want, _, bound = pu.forward64(p)
+    pu.near(tb.tb_packed_linear(w, p["x"].cuda())[0], want, bound, "y")
+    pu.near(tb.tb_packed_linear_backward(w, p["dy"].cuda())[0], *pu.backward64(p)["dx"], "dx")
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4, 7, 8])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n_tok", [5, 97, 1100])
+def test_zero_points_far_away(bits, dtype, n_tok):
+    """Differences beyond 256 are rounded to bf16: of a code and the zero-point's first piece, of that and the second, and with two bits of
+    the first piece less 120: two or three roundings, each off by 2^-8 of the difference at most (and a float's, 2^-23, where the zero-point
+    has more than 24 bits)."""
+    tb = _tb()
+    p = pu.problem(bits, n_tok, 264, 256, bits, 128, dtype)
+    g = torch.Generator().manual_seed(bits)
+    far = torch.cat([torch.randint(257, 5000, (100, 2), generator=g), torch.randint(-5000, -257, (100, 2), generator=g),
+                     torch.tensor([[5000001, -5000001], [8388607, -8388609], [16777217, -16777219], [2147483647, -2147483648]])])
+    z = p["zeros"].clone()
+    z[:204] = far.to(torch.int32)
+    p = _with_zero_points(p, z)
+    near = p["scales"] / (1 + 0.01 * z.double().abs()).float()    # so that no row drowns the others
+    p["Q"] = p["Q"] * (near.double() / p["scales"].double()).repeat_interleave(128, 1)
+    p["scales"] = near
+    w, _ = pu.on_gpu(tb, p)
+    far = (3.03 if bits == 2 else 2.02) * 2.0 ** -8
+    size = p["x"].double().abs() @ p["Q"].abs().T
+    want, _, bound = pu.forward64(p)
+    pu.near(tb.tb_packed_linear(w, p["x"].cuda())[0], want, bound + far * size, "y")
+    want, bound = pu.backward64(p)["dx"]
+    pu.near(tb.tb_packed_linear_backward(w, p["dy"].cuda())[0], want, bound + far * (p["dy"].double().abs() @ p["Q"].abs()), "dx")
+
+
 @pytest.mark.parametrize("rows,d,bits,group,n_tok", [(1032, 544, 4, 32, 70), (2056, 1024, 2, 128, 300), (4104, 256, 8, 0, 40), (520, 1152, 7, 384, 700), (8, 160, 3, 32, 5),
                                                      (72, 160, 5, 32, 33), (200, 128, 6, 0, 1100)])
 def test_input_gradient_with_all_of_the_weights(rows, d, bits, group, n_tok):
