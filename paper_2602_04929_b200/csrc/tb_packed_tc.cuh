@@ -17,7 +17,8 @@
 //
 // Adapters.  scale v M, v [tokens][rank] float, joins the sum as further contraction steps: slots of 16 for a run of tokens with one
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
-// into the tile as zero and is added by the epilogue to the run's own tokens, so that it reaches no other token.
+// into the tile as 2^-126 of its sign (an infinite v so comes to the infinity that it should) and is added by the epilogue to the run's own
+// tokens, so that it reaches no other token.
 //
 // Roles: warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and
 // scales, then the decode warps (forward two warpgroups, backward four, in turn), then the epilogue (forward eight warps, backward
@@ -560,8 +561,8 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             for (int i = 0; i < 4; ++i)
               if (not_finite2(o[i])) {
                 odd = true;
-                if ((o[i] & 0x7f80u) == 0x7f80u) o[i] &= 0xffff0000u;
-                if ((o[i] & 0x7f800000u) == 0x7f800000u) o[i] &= 0xffffu;
+                if ((o[i] & 0x7f80u) == 0x7f80u) o[i] = (o[i] & 0xffff8000u) | 0x0080u;
+                if ((o[i] & 0x7f800000u) == 0x7f800000u) o[i] = (o[i] & 0x8000ffffu) | 0x00800000u;
               }
             sts16(sa + (uint32_t)hf * 8192u + (uint32_t)kk * 128u + (((uint32_t)ch ^ (uint32_t)(kk & 7)) << 4), o);
           }

@@ -174,6 +174,63 @@ def test_zero_points_far_away(bits, dtype, n_tok):
     pu.near(tb.tb_packed_linear_backward(w, p["dy"].cuda())[0], want, bound + far * (p["dy"].double().abs() @ p["Q"].abs()), "dx")
 
 
+@pytest.mark.parametrize("rank", [16, 64, 128])
+@pytest.mark.parametrize("n_req", [3, 600])
+@pytest.mark.parametrize("n_tok,rows,d", [(600, 520, 256), (2600, 264, 512)])
+def test_what_is_not_finite_in_tiles(rank, n_req, n_tok, rows, d):
+    """More than 2^18 results, so tiles, with the adapters in stages of their own (few requests, backward the larger shape) or joined to float
+    sums: an infinity or what is no number stays with its token or its adapter's requests, both ways, and an infinity that meets an
+    infinity is one."""
+    tb = _tb()
+    starts = [n_tok * k // n_req for k in range(n_req + 1)]
+    ids = [1, 0, 1] if n_req == 3 else [k % 3 - 1 for k in range(n_req)]
+    p = pu.problem(rank, n_tok, rows, d, 4, 128, BF, 3, rank, starts, ids)
+    own = pu.owners(p)
+    mine, others = (own == 0).nonzero().flatten().tolist(), own != 0
+    nan_tok, inf_tok = mine[1], mine[2]
+    # token inf_tok has an infinity at input column k (y's column 40) or at row j of dy (dx's column 50): all its terms are positive infinities
+    k, j = int((p["Q"][40, :50] > 0).nonzero()[0]), int((p["Q"][:40, 50] > 0).nonzero()[0])
+    g = torch.Generator().manual_seed(rank)
+    p["B"][0, :, 40] = p["A"][0, :, k].sign() * (0.1 + torch.rand(rank, generator=g)).to(BF)
+    p["A"][0, :, 50] = p["B"][0, :, j].sign() * (0.1 + torch.rand(rank, generator=g)).to(BF)
+    p["A"][2] = float("nan")                       # no request has this one
+    clean = {n: p[n].clone() for n in ("x", "dy", "A", "B")}
+    p["x"][nan_tok, 200], p["x"][inf_tok, k] = float("nan"), float("inf")
+    p["dy"][nan_tok, 5], p["dy"][inf_tok, j] = float("nan"), float("inf")
+    p["B"][0, 3, 40] = float("inf") * p["B"][0, 3, 40].sign()
+    w, a = pu.on_gpu(tb, p)
+    y, xa = (v.cpu() for v in tb.tb_packed_linear(w, p["x"].cuda(), a))
+    good = dict(p, **clean)
+    want, xa64, bound = pu.forward64(good)
+    fine = torch.ones(n_tok, dtype=torch.bool)
+    fine[[nan_tok, inf_tok]] = False
+    cols = torch.ones(rows, dtype=torch.bool)
+    cols[40] = False
+    pu.near(y[fine][:, cols], want[fine][:, cols], bound[fine][:, cols], "y")
+    pu.near(y[fine & others], want[fine & others], bound[fine & others], "y of other requests")
+    assert not torch.isfinite(y[~others][:, 40]).any() and torch.isnan(y[nan_tok]).all()
+    assert torch.isinf(xa[inf_tok]).all() and torch.isnan(xa[nan_tok]).all() and torch.isfinite(xa[fine]).all()
+    assert y[inf_tok, 40] == float("inf")
+    one = mine[5]                                  # a finite token of the request: the sign is that of its low value
+    assert y[one, 40] == float("inf") * (xa64[one, 3] * p["B"][0, 3, 40].double()).sign()
+    # backward, with an infinity in A
+    q = dict(good, dy=p["dy"], A=clean["A"].clone())
+    q["A"][0, 2, 50] = float("inf") * q["A"][0, 2, 50].sign()
+    w, a = pu.on_gpu(tb, q)
+    dx, dA, dB = (v.cpu() for v in tb.tb_packed_linear_backward(w, q["dy"].cuda(), a, x=good["x"].cuda(), xa=xa64.float().cuda()))
+    ref = pu.backward64(good, None, xa64.float())
+    cols = torch.ones(d, dtype=torch.bool)
+    cols[50] = False
+    pu.near(dx[fine][:, cols], ref["dx"][0][fine][:, cols], ref["dx"][1][fine][:, cols], "dx")
+    pu.near(dx[fine & others], ref["dx"][0][fine & others], ref["dx"][1][fine & others], "dx of other requests")
+    assert not torch.isfinite(dx[~others][:, 50]).any() and torch.isnan(dx[nan_tok]).all()
+    assert dx[inf_tok, 50] == float("inf")
+    for got, name in ((dA, "dA"), (dB, "dB")):
+        pu.near(got[1], ref[name][0][1], ref[name][1][1], name)
+        assert not got[2].any()
+    assert tb.tb_device_error_flag() == 0
+
+
 @pytest.mark.parametrize("rows,d,bits,group,n_tok", [(1032, 544, 4, 32, 70), (2056, 1024, 2, 128, 300), (4104, 256, 8, 0, 40), (520, 1152, 7, 384, 700), (8, 160, 3, 32, 5),
                                                      (72, 160, 5, 32, 33), (200, 128, 6, 0, 1100)])
 def test_input_gradient_with_all_of_the_weights(rows, d, bits, group, n_tok):
