@@ -19,6 +19,10 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
 
 static __device__ int g_grad_error = 0;
 
+// Columns of an accumulation of x A_i^T at most: every step of 16 may drop the last bits of the sum, always to one side.  In one sum,
+// 8192 columns are 2.1e-6 off and 65536 are 1.9e-5; in sums of 512 added in float, 4.7e-7 and 5.2e-7.
+enum { LOW_PART = 512 };
+
 // ------------------------------------------------------------------------------------------ x A_i^T
 //
 // For few tokens, on mma.sync: a CTA has 16 tokens, one of the adapters that they have, up to 64 of its rank and, as one of a cluster,
@@ -71,20 +75,32 @@ __global__ void __launch_bounds__(256) k_adapter_low(Adapt ad, const __nv_bfloat
   float acc[NT][4] = {};
   const int steps = (width + 31) / 32, per = (steps + (int)cs * KG - 1) / ((int)cs * KG);
   const int s0 = ((int)rank * KG + warp) * per, s1 = min(steps, s0 + per);
+  auto add = [&](float (&to)[NT][4], int from, int end) {
 #pragma unroll 4
-  for (int s = s0; s < s1; ++s) {
-    const int k = 32 * s + 8 * q;
-    const bool in_k = k < width;
-    uint4 x[2], m[NT];
+    for (int s = from; s < end; ++s) {
+      const int k = 32 * s + 8 * q;
+      const bool in_k = k < width;
+      uint4 x[2], m[NT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = in_k && xr[i] ? *reinterpret_cast<const uint4*>(xr[i] + k) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 2; ++i) x[i] = in_k && xr[i] ? *reinterpret_cast<const uint4*>(xr[i] + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) m[n] = in_k && mr[n] ? *reinterpret_cast<const uint4*>(mr[n] + k) : make_uint4(0, 0, 0, 0);
+      for (int n = 0; n < NT; ++n) m[n] = in_k && mr[n] ? *reinterpret_cast<const uint4*>(mr[n] + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      mma_bf16(acc[n], x[0].x, x[1].x, x[0].y, x[1].y, m[n].x, m[n].y);
-      mma_bf16(acc[n], x[0].z, x[1].z, x[0].w, x[1].w, m[n].z, m[n].w);
+      for (int n = 0; n < NT; ++n) {
+        mma_bf16(to[n], x[0].x, x[1].x, x[0].y, x[1].y, m[n].x, m[n].y);
+        mma_bf16(to[n], x[0].z, x[1].z, x[0].w, x[1].w, m[n].z, m[n].w);
+      }
     }
+  };
+  constexpr int PART = LOW_PART / 32;
+  add(acc, s0, min(s1, s0 + PART));  // most calls end here, without a second set of sums
+  for (int p0 = s0 + PART; p0 < s1; p0 += PART) {
+    float more[NT][4] = {};
+    add(more, p0, min(s1, p0 + PART));
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[n][c] += more[n][c];
   }
   // the warps along the contraction, one after the other
   for (int k = 0; k < KG; ++k) {
@@ -147,29 +163,33 @@ static tb_status launch_low(const Adapt& ad, const __nv_bfloat16* in, const __nv
 // The same for many tokens, on tcgen05: 128 tokens are the rows M of the tile, the rank its columns N, both operands by TMA as they
 // are stored (K-major).  x so is read once, at HBM's rate, and an adapter once for 128 tokens.  A tile's adapters (AL_COLS / N of
 // them, more in further CTAs) are gone through one after the other, each into columns of its own; rows of other adapters are computed and
-// dropped.  CTAs of a cluster share the contraction; an accumulation ends after 512 columns where tensor memory has room for more of
-// them (every step may drop the last bit).
+// dropped.  CTAs of a cluster share the contraction; an accumulation ends after LOW_PART columns.  Where tensor memory has not room for all
+// of them (the CTA then has one adapter), they are added to registers as often as it is full, and the products go on from its beginning.
 //
 // 8192 x 4096, rank 16: 22 us (67 MB at 3.0 TB/s); 4099 x 8192, rank 64: 33 us (67 MB at 2.0 TB/s).  A tile is loaded, multiplied and
 // written by one CTA an SM in turn, so that neither end of it overlaps with another tile's loads.
 
-enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_PART = 512, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
+enum { AL_TOK = 128, AL_BK = 64, AL_COLS = 512, AL_THREADS = 192, AL_ROOM = 200 * 1024 };
 
 struct LowTc {
   Adapt ad;
   float* low;
-  int n_tok, width, n, stages, per, part, n_parts;  // n: the rank rounded up to 16; per: contraction columns of a CTA
+  // n: the rank rounded up to 16; per: contraction columns of a CTA; part: stages of an accumulation, n_parts: those of an adapter that
+  // tensor memory holds at a time
+  int n_tok, width, n, stages, per, part, n_parts;
 };
 
+// ROUNDS: tensor memory fills more than once
+template <bool ROUNDS>
 __global__ void __launch_bounds__(AL_THREADS, 1)
     k_adapter_low_tc(const __grid_constant__ LowTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap mmap) {
   extern __shared__ unsigned char al_raw[];
-  __shared__ __align__(8) unsigned long long bars[2 * 16 + 1];
+  __shared__ __align__(8) unsigned long long bars[2 * 16 + 2];
   __shared__ uint32_t tmem_slot;
   __shared__ int gave_up, own[AL_TOK], cand[AL_TOK], firsts[4], n_ids;
   const uint32_t base = (smem_u32(al_raw) + 1023u) & ~1023u;
   float* sums = reinterpret_cast<float*>(al_raw + (base - smem_u32(al_raw)));  // after the last stage: [128][n + 1]
-  const uint32_t bar0 = smem_u32(bars), done_bar = bar0 + 8u * 32;
+  const uint32_t bar0 = smem_u32(bars), done_bar = bar0 + 8u * 32, read_bar = bar0 + 8u * 33;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (16 + s); };
   uint32_t rank, cs;
@@ -182,6 +202,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
       mbar_init(empty_bar(s), 1);
     }
     mbar_init(done_bar, 1);
+    mbar_init(read_bar, 4);
     gave_up = 0;
     mbar_fence_init();
   }
@@ -225,6 +246,29 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
   const uint32_t tmem = tmem_slot;
   const int stage_bytes = AL_TOK * 128 + p.n * 128;  // a multiple of 1024: n is one of 16, hence of 8 rows of 128 bytes
   const int k0 = (int)rank * p.per, k1 = min(p.width, k0 + p.per), n_st = k1 > k0 ? (k1 - k0 + AL_BK - 1) / AL_BK : 0;
+  const int full = p.part * p.n_parts, rounds = ROUNDS && n_st > full ? (n_st + full - 1) / full : 1;  // stages that fill tensor memory
+  float total[ROUNDS ? 128 : 1];  // warps 0 to 3: a token's sums of the rounds but the last
+  if (ROUNDS && warp < 4) {
+#pragma unroll
+    for (int i = 0; i < (ROUNDS ? 128 : 1); ++i) total[i] = 0.0f;
+    for (int round = 0; round + 1 < rounds; ++round) {
+      if (!__all_sync(0xffffffffu, mbar_wait(done_bar, round & 1u, &gave_up, &g_grad_error))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      for (int part = 0; part < p.n_parts; ++part)
+#pragma unroll
+        for (int c = 0; c < 128; c += 8) {
+          if (c >= p.n) break;
+          uint32_t r[8];
+          tmem_ld_32x8(tmem + ((uint32_t)(warp * 32) << 16) + (uint32_t)(part * p.n + c), r);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+          for (int i = 0; i < 8; ++i) total[ROUNDS ? c + i : 0] += __uint_as_float(r[i]);
+        }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(read_bar);
+    }
+  }
   if (warp == 4 && lane == 0) {
     int s = 0;
     uint32_t phase = 1;
@@ -247,7 +291,7 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
     uint32_t phase = 0;
     bool ok = true;
     for (int a = 0; a < ids && ok; ++a) {
-      int in_part = 0, part = 0;
+      int in_part = 0, part = 0, round = 0;
       for (int st = 0; st < n_st; ++st) {
         ok = __all_sync(0xffffffffu, mbar_wait(full_bar(s), phase, &gave_up, &g_grad_error));
         if (!ok) break;
@@ -262,24 +306,36 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
         __syncwarp();
         if (++in_part == p.part) in_part = 0, ++part;
         if (++s == p.stages) s = 0, phase ^= 1u;
+        if (ROUNDS && part == p.n_parts && st + 1 < n_st) {  // full: from its beginning again, once these have been read
+          if (one) umma_commit(done_bar);
+          __syncwarp();
+          ok = __all_sync(0xffffffffu, mbar_wait(read_bar, round & 1u, &gave_up, &g_grad_error));
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          part = 0, ++round;
+        }
       }
     }
     if (one) umma_commit(done_bar);
   }
   __syncthreads();
-  bool ok = __all_sync(0xffffffffu, mbar_wait(done_bar, 0, &gave_up, &g_grad_error));
+  bool ok = __all_sync(0xffffffffu, mbar_wait(done_bar, (rounds - 1) & 1u, &gave_up, &g_grad_error));
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   // a thread of the first four warps has a token, whose sums are in the columns of its adapter
   const uint32_t mine = smem_u32(sums);
-  const int pitch = p.n + 1, parts_here = ok ? (n_st + p.part - 1) / p.part : 0;
+  const int pitch = p.n + 1, parts_here = ok ? (n_st - (rounds - 1) * full + p.part - 1) / p.part : 0;
   if (warp < 4) {
     bool here = false;
     for (int a = 0; a < ids; ++a) {
       const bool own_row = own[tid] == cand[id0 + a];
       if (!__any_sync(0xffffffffu, own_row)) continue;
       here = here || own_row;
-      for (int c = 0; c < p.n; c += 32) {
-        float v[32] = {};
+#pragma unroll(ROUNDS ? 4 : 1)
+      for (int c = 0; c < 128; c += 32) {
+        if (c >= p.n) break;
+        float v[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = ROUNDS ? total[ROUNDS ? c + i : 0] : 0.0f;
         for (int part = 0; part < parts_here; ++part) {
           uint32_t r[4][8];
 #pragma unroll
@@ -325,34 +381,18 @@ __global__ void __launch_bounds__(AL_THREADS, 1)
   if (warp == 5) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)AL_COLS) : "memory");
 }
 
-static tb_status launch_low_tc(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, cudaStream_t st) {
+template <bool ROUNDS>
+static tb_status launch_low_tc(const LowTc& p, const CUtensorMap& xmap, const CUtensorMap& mmap, unsigned x, unsigned y, int cs, cudaStream_t st) {
   static bool configured[64] = {false};
   int dev = 0;
   TB_CUDA_CHECK(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return TB_ERR_CUDA;
   if (!configured[dev]) {
-    TB_CUDA_CHECK(cudaFuncSetAttribute(k_adapter_low_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, AL_ROOM + 1024));
+    TB_CUDA_CHECK(cudaFuncSetAttribute(k_adapter_low_tc<ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, AL_ROOM + 1024));
     configured[dev] = true;
   }
-  const int tiles = (n_tok + AL_TOK - 1) / AL_TOK, sms = sm_count() > 0 ? sm_count() : 148;
-  int cs = 1;  // CTAs along the contraction, up to one an SM
-  while (cs < 8 && tiles * cs * 2 <= sms && width / (2 * cs) >= 256) cs *= 2;
-  LowTc p;
-  p.ad = ad, p.low = low, p.n_tok = n_tok, p.width = width;
-  p.n = (ad.rank + 15) / 16 * 16;
-  p.per = ((width + cs - 1) / cs + AL_BK - 1) / AL_BK * AL_BK;
-  p.n_parts = min((p.per + AL_PART - 1) / AL_PART, AL_COLS / p.n);
-  p.part = ((p.per / AL_BK) + p.n_parts - 1) / p.n_parts;
-  const int stage = AL_TOK * 128 + p.n * 128;
-  p.stages = min(12, AL_ROOM / stage);
-  const int ys = (min(AL_TOK, min(ad.n_req, ad.n)) + AL_COLS / (p.n * p.n_parts) - 1) / (AL_COLS / (p.n * p.n_parts));
-  CUtensorMap xmap, mmap;
-  TB_TRY(make_map_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, in, (unsigned long long)width, (unsigned long long)n_tok, AL_BK, AL_TOK,
-                     CU_TENSOR_MAP_SWIZZLE_128B));
-  TB_TRY(make_map_2d(&mmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, M, (unsigned long long)width, (unsigned long long)ad.n * ad.rank, AL_BK, p.n,
-                     CU_TENSOR_MAP_SWIZZLE_128B));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * cs), (unsigned)ys);
+  cfg.gridDim = dim3(x, y);
   cfg.blockDim = dim3(AL_THREADS);
   cfg.dynamicSmemBytes = AL_ROOM + 1024;  // no second CTA that would wait for tensor memory
   cfg.stream = st;
@@ -363,9 +403,31 @@ static tb_status launch_low_tc(const Adapt& ad, const __nv_bfloat16* in, const _
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low_tc, p, xmap, mmap));
+  TB_CUDA_CHECK(cudaLaunchKernelEx(&cfg, k_adapter_low_tc<ROUNDS>, p, xmap, mmap));
   TB_LAUNCH_CHECK();
   return TB_OK;
+}
+
+static tb_status adapter_low_tc(const Adapt& ad, const __nv_bfloat16* in, const __nv_bfloat16* M, int n_tok, int width, float* low, cudaStream_t st) {
+  const int tiles = (n_tok + AL_TOK - 1) / AL_TOK, sms = sm_count() > 0 ? sm_count() : 148;
+  int cs = 1;  // CTAs along the contraction, up to one an SM
+  while (cs < 8 && tiles * cs * 2 <= sms && width / (2 * cs) >= 256) cs *= 2;
+  LowTc p;
+  p.ad = ad, p.low = low, p.n_tok = n_tok, p.width = width;
+  p.n = (ad.rank + 15) / 16 * 16;
+  p.per = ((width + cs - 1) / cs + AL_BK - 1) / AL_BK * AL_BK;
+  p.n_parts = min((p.per + LOW_PART - 1) / LOW_PART, AL_COLS / p.n);
+  p.part = min(LOW_PART / AL_BK, (p.per / AL_BK + p.n_parts - 1) / p.n_parts);
+  const int stage = AL_TOK * 128 + p.n * 128;
+  p.stages = min(12, AL_ROOM / stage);
+  const int ys = (min(AL_TOK, min(ad.n_req, ad.n)) + AL_COLS / (p.n * p.n_parts) - 1) / (AL_COLS / (p.n * p.n_parts));
+  CUtensorMap xmap, mmap;
+  TB_TRY(make_map_2d(&xmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, in, (unsigned long long)width, (unsigned long long)n_tok, AL_BK, AL_TOK,
+                     CU_TENSOR_MAP_SWIZZLE_128B));
+  TB_TRY(make_map_2d(&mmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, M, (unsigned long long)width, (unsigned long long)ad.n * ad.rank, AL_BK, p.n,
+                     CU_TENSOR_MAP_SWIZZLE_128B));
+  const unsigned x = (unsigned)(tiles * cs), y = (unsigned)ys;
+  return p.per / AL_BK > p.part * p.n_parts ? launch_low_tc<true>(p, xmap, mmap, x, y, cs, st) : launch_low_tc<false>(p, xmap, mmap, x, y, cs, st);
 }
 
 // Tiles of 16 tokens start sooner and compute less for rows of other adapters, but read an adapter once for every 16 tokens.
@@ -387,7 +449,7 @@ tb_status adapter_low_bf16(const Adapt& ad, const __nv_bfloat16* in, const __nv_
     if (ad.rank <= 32) return launch_low<4>(ad, in, M, n_tok, width, low, st, late);
     return launch_low<8>(ad, in, M, n_tok, width, low, st, late);
   }
-  return launch_low_tc(ad, in, M, n_tok, width, low, st);
+  return adapter_low_tc(ad, in, M, n_tok, width, low, st);
 }
 
 // ------------------------------------------------------------------------------------------ gradients

@@ -267,3 +267,31 @@ def test_an_infinite_gradient_meets_the_weights(bits, group, n_tok):
     assert torch.isnan(dx[2]).all()
     want, bound = pu.backward64(dict(p, dy=clean))["dx"]
     pu.near(dx[3:], want[3:], bound[3:], "dx") if n_tok > 3 else None
+
+
+@pytest.mark.parametrize("n_tok,d,rank,n_req", [(16, 524288, 16, 2), (2048, 524288, 64, 2), (5000, 65536, 128, 1), (5000, 65536, 48, 3), (300, 100032, 8, 2), (40, 65536, 128, 7),
+                                                (2600, 10240, 112, 2), (1300, 33344, 40, 5)])
+def test_sums_of_the_narrow_product(n_tok, d, rank, n_req):
+    """No accumulation of x A^T is longer than 512 columns, whatever the rank, the width and the kernel.  A step of 16 columns drops at most
+    2^-23 of the sum that it adds to, which on the way to 512 columns averages 2/3 of the sum of 512 (it grows like a root): 32 steps.
+    Neighbouring sums have nothing to do with one another; the d / 512 additions that join them round to the nearest, to either side,
+    2^-24 each at most, so the root of their number in the norm."""
+    tb = _tb()
+    p = pu.problem(5, 1, 8, 32, 2, 0, BF, 3, rank, [0, 1], [0])
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    w = tb.packed_weight(ints(8, d // 16), torch.ones((8, 1), device="cuda"), ints(8, 1), d, 2)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((n_tok, d), generator=g, device="cuda").to(BF)
+    A = (torch.randn((3, rank, d), generator=g, device="cuda") / d ** 0.5).to(BF)
+    cuts = [n_tok * k // n_req for k in range(n_req + 1)]
+    ids = [k % 3 for k in range(n_req)]
+    _, xa = tb.tb_packed_linear(w, x, tb.adapters(A, p["B"].cuda(), p["scale"].cuda(), torch.tensor(cuts, dtype=torch.int32).cuda(),
+                                                  torch.tensor(ids, dtype=torch.int32).cuda()))
+    off, size = 0.0, 0.0
+    for j, i in enumerate(ids):
+        for t in range(cuts[j], cuts[j + 1], 512):   # some of them, so that the doubles fit
+            s = slice(t, min(t + 64, cuts[j + 1]))
+            want = x[s].double() @ A[i].double().T
+            off, size = off + float((xa[s] - want).square().sum()), size + float(want.square().sum())
+    assert (off / size) ** 0.5 <= 2 / 3 * 32 * 2.0 ** -23 + (d / 512) ** 0.5 * 2.0 ** -24
+    assert tb.tb_device_error_flag() == 0
