@@ -210,12 +210,12 @@ using namespace tb;
 static tb_status checkpoint_shape(tb_dtype type, long long n_tok, int d, const void* x, const void* codes,
                                   const void* scales, long long* n_runs, unsigned* blocks, unsigned long long* per_inv) {
   if ((type != TB_F32 && type != TB_BF16) || n_tok < 0 || d <= 0) return TB_ERR_INVALID_ARG;
-  if (d % 32) return TB_ERR_UNSUPPORTED;
-  *n_runs = n_tok * ((d + CKPT_RUN - 1) / CKPT_RUN);
-  const unsigned long long n_g = (unsigned)(d + CKPT_RUN - 1) / CKPT_RUN;
-  *per_inv = n_g > 1 ? ~0ull / n_g + 1 : 0;
+  if (d % 32 || n_tok > 0x7fffffffll) return TB_ERR_UNSUPPORTED;
+  const long long n_g = ((long long)d + CKPT_RUN - 1) / CKPT_RUN;  // d may be 2^31 - 32
+  *n_runs = n_tok * n_g;
+  *per_inv = n_g > 1 ? ~0ull / (unsigned long long)n_g + 1 : 0;
   const long long nb = (*n_runs + 16 * CKPT_PER - 1) / (16 * CKPT_PER);
-  if (n_tok > 0x7fffffffll || nb > 0x7fffffffll) return TB_ERR_UNSUPPORTED;
+  if (nb > 0x7fffffffll) return TB_ERR_UNSUPPORTED;
   *blocks = (unsigned)nb;
   if (n_tok == 0) return TB_OK;
   if (!x || !codes || !scales) return TB_ERR_INVALID_ARG;
@@ -230,7 +230,7 @@ extern "C" tb_status tb_checkpoint_pack(const void* x, tb_dtype x_type, long lon
   unsigned long long per_inv;
   TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb, &per_inv));
   if (nb == 0) return TB_OK;
-  const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
+  const int n_g = (int)(((long long)d + CKPT_RUN - 1) / CKPT_RUN);
   if (x_type == TB_BF16)
     k_checkpoint_pack<<<nb, 256, 0, as_stream(stream)>>>(static_cast<const __nv_bfloat16*>(x), codes, scales, n_runs, d, n_g, per_inv);
   else
@@ -246,7 +246,7 @@ extern "C" tb_status tb_checkpoint_unpack(const signed char* codes, const float*
   unsigned long long per_inv;
   TB_TRY(checkpoint_shape(x_type, n_tok, d, x, codes, scales, &n_runs, &nb, &per_inv));
   if (nb == 0) return TB_OK;
-  const int n_g = (d + CKPT_RUN - 1) / CKPT_RUN;
+  const int n_g = (int)(((long long)d + CKPT_RUN - 1) / CKPT_RUN);
   if (x_type == TB_BF16)
     k_checkpoint_unpack<<<nb, 256, 0, as_stream(stream)>>>(codes, scales, static_cast<__nv_bfloat16*>(x), n_runs, d, n_g, per_inv);
   else

@@ -295,3 +295,20 @@ def test_sums_of_the_narrow_product(n_tok, d, rank, n_req):
             off, size = off + float((xa[s] - want).square().sum()), size + float(want.square().sum())
     assert (off / size) ** 0.5 <= 2 / 3 * 32 * 2.0 ** -23 + (d / 512) ** 0.5 * 2.0 ** -24
     assert tb.tb_device_error_flag() == 0
+
+
+def test_8_bit_form_of_the_widest_token():
+    """A token of 2^31 - 32 values, its last run a short one: counts of runs and columns stay within what holds them."""
+    tb = _tb()
+    d = (1 << 31) - 32
+    x = torch.empty((1, d), dtype=BF, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x.normal_(generator=g)
+    codes, scales = tb.tb_checkpoint_pack(x)
+    assert scales.shape == (1, 1 << 24)
+    back = tb.tb_checkpoint_unpack(codes, scales, BF)
+    for s in (slice(0, 4096), slice((1 << 30) - 1024, (1 << 30) + 1024), slice((1 << 31) - 4096, d)):
+        part = x[:, s].clone()
+        c, k = tb.tb_checkpoint_pack(part)
+        assert torch.equal(codes[:, s], c) and torch.equal(scales[:, s.start // 128:-(-s.stop // 128)], k)
+        assert torch.equal(back[:, s], tb.tb_checkpoint_unpack(c, k, BF))
