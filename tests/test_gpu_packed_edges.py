@@ -297,6 +297,53 @@ def test_sums_of_the_narrow_product(n_tok, d, rank, n_req):
     assert tb.tb_device_error_flag() == 0
 
 
+@pytest.mark.parametrize("n_tok,rows,d,bits,group,rank", [(208, 832, 2688, 4, 128, 128), (40, 136, 384, 4, 128, 8), (300, 1160, 128, 3, 0, 16), (70, 264, 640, 8, 128, 8),
+                                                        (1100, 264, 384, 2, 384, 8), (90, 200, 96, 5, 96, 16), (24, 136, 1152, 7, 128, 16), (1, 8, 32, 2, 32, 8), (5, 40, 160, 3, 32, 24)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_what_lies_behind_the_inputs_is_not_read(n_tok, rows, d, bits, group, rank, dtype):
+    """Every input starts where its alignment just allows it and is followed, without a gap, by values that would show: infinite
+    or undefined floats, huge integers.  Outputs, gradients of both forms of the input among them, are right, and the same bits
+    whichever values follow."""
+    tb = _tb()
+
+    def between(v, word, align):
+        n = v.numel() * v.element_size()
+        room = torch.full((4096 + n // 4 + 4096,), word, dtype=torch.int32, device="cuda").view(torch.uint8)
+        to = room[16384 + align:][:n].view(v.dtype).view(v.shape)
+        to.copy_(v)
+        return to
+
+    p = pu.problem(n_tok + rows, n_tok, rows, d, bits, group, dtype, 2, rank, sorted([0, n_tok // 3, n_tok // 2, n_tok]), [1, 0, 1])
+    w0, a0 = pu.on_gpu(tb, p)
+    xa64 = pu.forward64(p)[1].float()
+    codes0, scales0 = (torch.from_numpy(v).cuda() for v in pu.eight_bits(p["x"]))
+    runs = []
+    for word in (0x7f807f80, 0x7fc07fc0, 0x01010101):       # infinities, no numbers, small numbers
+        w = tb.packed_weight(*(between(v, word, k) for v, k in zip(w0.tensors, (16, 4, 4))), d, bits, group)
+        a = tb.adapters(*(between(v, word, k) for v, k in zip(a0.tensors, (16, 16, 4, 4, 4))))
+        x, dy, xa, codes = (between(v.cuda(), word, 16) for v in (p["x"], p["dy"], xa64, codes0))
+        scales = between(scales0, word, 4)
+        out = [*tb.tb_packed_linear(w, x, a), tb.tb_packed_linear(w, x)[0], *tb.tb_checkpoint_pack(x), tb.tb_checkpoint_unpack(codes, scales, dtype)]
+        for kept in (dict(x=x), dict(checkpoint=(codes, scales))):
+            out += tb.tb_packed_linear_backward(w, dy, a, xa=xa, **kept)
+        runs.append(out)
+    for other in runs[1:]:
+        assert all(torch.equal(u, v) for u, v in zip(runs[0], other))
+    y, _, plain, codes, scales, _, *grads = runs[0]
+    want, _, bound = pu.forward64(p)
+    pu.near(y, want, bound, "y")
+    bare = {k: v for k, v in p.items() if k != "ids"}
+    want, _, bound = pu.forward64(bare)
+    pu.near(plain, want, bound, "plain")
+    assert torch.equal(codes, codes0) and torch.equal(scales, scales0)
+    x8 = codes0.double().cpu() * scales0.double().cpu().repeat_interleave(128, 1)[:, :d]
+    for got, inp in ((grads[:3], None), (grads[3:], x8)):
+        ref = pu.backward64(p, inp, xa64)
+        for v, name in zip(got, ("dx", "dA", "dB")):
+            pu.near(v, *ref[name], name)
+    assert tb.tb_device_error_flag() == 0
+
+
 def test_8_bit_form_of_the_widest_token():
     """A token of 2^31 - 32 values, its last run a short one: counts of runs and columns stay within what holds them."""
     tb = _tb()
