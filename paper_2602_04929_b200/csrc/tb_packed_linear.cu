@@ -79,7 +79,11 @@ tb_status packed_few_f32_2(const PackedFew& p, cudaStream_t st);
 // 14.4 / 17.1, 32.2 / 31.2; 48 tokens 20.5 / 17.5, 46.7 / 32.0.  Smaller weights, 4 bits (us in a graph): 2048 x 2048, 64 tokens
 // 9.1 / 12.5, 96 tokens 12.8 / 12.7; 1024 x 4096, 64 tokens 11.1 / 12.9, 96 tokens 15.9 / 12.6; 1024 x 1024, 128 tokens 6.9 / 10.9,
 // 256 tokens 9.3 / 11.8; 2048 x 512, 128 tokens 7.9 / 9.7, 256 tokens 14.5 / 10.3; 512 x 512, 512 tokens 7.9 / 9.5, 1023 tokens 14.3 /
-// 10.2.  The adapters' share is computed per 16 tokens here: rank 16, 1024 x 1024, 256 tokens 18.4 / 20.5; rank 64, 512 x 512, 128
+// 10.2.  The adapters' share is computed per 16 tokens here, from rows that each of its outputs reads, so that tokens x columns x rank decides
+// from nine tokens on (4 bits, requests of a token each): 4096 x 4096, 16 tokens, rank 64 23.0 / 29.3, rank 128 39.3 / 35.0; 32 tokens,
+// rank 16 24.0 / 23.2, rank 64 36.7 / 30.5, rank 128 50.7 / 36.2; 8192 x 512, 32 tokens, rank 16 16.7 / 17.3, rank 128 51.6 / 39.5; 8192 x 8192,
+// 2 bits, 32 tokens, rank 128 82 / 58; 1024 x 1024, 32 tokens, rank 128 22.6 / 24.8; with eight tokens 8192 x 8192, rank 128 30.8 / 50.9,
+// 512 x 8192 21.2 / 27.4.  Work of more tokens: rank 16, 1024 x 1024, 256 tokens 18.4 / 20.5; rank 64, 512 x 512, 128
 // tokens 19.1 / 44, 512 tokens 35.7 / 32.6; rank 128, 512 x 512, 64 tokens 14.7 / 33.4, 256 tokens 36.0 / 32.7, 8192 x 512, 64 tokens
 // 100 / 35.
 // Float, 4 bits, registers / tiles: 4096 x 4096, 64 tokens 61 / 85, 128 tokens 104 / 85, 1024 tokens 784 / 603; 8192 x 8192, 128 tokens
@@ -89,7 +93,8 @@ static bool takes_few(const PackedW& w, const Adapt& ad, tb_dtype type, long lon
   if (back) return false;
   if (type == TB_F32) return n_tok <= FEW_TOKENS_F32;
   const long long outputs = n_tok * w.d_out, ranks = ad.n && ad.rank > 16 ? ad.rank : 16;  // n_tok < 2^30, d_out <= 2^24
-  return n_tok <= FEW_TOKENS || (outputs * ranks <= FEW_OUTPUTS * 16ll && outputs * w.d_in <= FEW_WORK);
+  if (n_tok <= 8 || (n_tok <= FEW_TOKENS && !ad.n)) return true;
+  return outputs * ranks <= FEW_OUTPUTS * 16ll && (n_tok <= FEW_TOKENS || outputs * w.d_in <= FEW_WORK);
 }
 
 // Scratch of a call: the product's own, and for the backward pass u = dy B^T of every token, not scaled.
