@@ -363,8 +363,8 @@ tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapter
  * as x_codes and x_scales from tb_checkpoint_pack; xa is the forward pass's.  x, codes
  * and xa may be NULL without dA.  dy [n_tok][d_out] of x_type.  n_tok may be 0, with any
  * array of tokens NULL, dx among them.
- * In bf16 the weights enter dx as two pieces of bf16, 2^-16 of a weight off in the mean and
- * 2^-13 at most. */
+ * In bf16 the weights enter dx as two pieces of bf16, 2^-17 of a weight off in the mean and
+ * 2^-13.9 at most. */
 size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
                                            tb_dtype x_type, long long n_tok);
 tb_status tb_packed_linear_backward(const tb_packed_weight* w, const tb_adapters* adapters,

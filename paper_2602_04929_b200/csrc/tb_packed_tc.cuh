@@ -11,7 +11,7 @@
 // holds c - z, which bf16 has exactly, and the accumulator of a group (at most 2048 columns of it) is taken from one of two TMEM
 // buffers, scaled and added to float registers by the epilogue warps while the other buffer fills.  The product so has no rounding
 // but that of float sums.  Backward, a scale belongs to the contraction row, so the weight s (c - z) itself is decoded, as two pieces
-// of bf16 (scale8: 2^-16 of the weight in the mean, 2^-13 at most; a single piece would put as large an error on dx as its own rounding
+// of bf16 (scale8: 2^-17 of the weight in the mean, 2^-13.9 at most; a single piece would put as large an error on dx as its own rounding
 // does).  Each piece is a stage of its own with the same tokens, twice the products of a single one, and the sum stays in tensor memory
 // to its end, one buffer a tile.
 //
@@ -74,22 +74,23 @@ struct Parts {
   }
 };
 
-// c - z, exact, times s, as two pieces of bf16; s comes in two as well, hi and lo.  The first piece is (c - z) s less about 2^-7 of it,
-// rounded; the second is what that leaves, 2^-9.5 to 2^-6.1 of the weight, so that both have the weight's sign and an infinite dy
-// comes to the infinity that it should (a remainder of either sign would give infinity less infinity).  (c - z) hi less the first piece is
-// exact for codes of four bits, else rounded like the second piece itself: at most 2^-14.1 of the weight each.
+// c - z, exact, times s, as two pieces of bf16; s comes in two as well, hi and lo.  The first piece is (c - z) s less a little more than
+// 2^-8 of it, half a step, rounded; the second is what that leaves, more than 0 and at most 2^-6.9 of the weight, so that both have the
+// weight's sign and an infinite dy comes to the infinity that it should (a remainder of either sign would give infinity less infinity).
+// (c - z) hi less the first piece is exact for codes of four bits, else rounded like the second piece itself: at most 2^-14.9 of the weight
+// each, 2^-17 in the mean.
 struct ScalePieces {
-  unsigned hi, lo, less;  // twice each
+  unsigned hi, lo, less;  // twice each; less: lo less 1.0625 2^-8 of hi
   __device__ __forceinline__ void set(unsigned v) {
     hi = __byte_perm(v, 0, 0x3232), lo = __byte_perm(v, 0, 0x1010);
-    less = bf2(__hmul2(bf2(hi), __float2bfloat162_rn(0.9921875f)));
+    less = bf2(__hfma2(bf2(hi), __float2bfloat162_rn(-0.004150390625f), bf2(lo)));
   }
 };
 template <int PIECE>
 __device__ __forceinline__ void scale8(unsigned (&o)[4], const ScalePieces& s) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 q = bf2(o[i]), first = __hfma2(q, bf2(s.less), __hmul2(q, bf2(s.lo)));
+    const __nv_bfloat162 q = bf2(o[i]), first = __hfma2(q, bf2(s.hi), __hmul2(q, bf2(s.less)));
     o[i] = bf2(PIECE == 0 ? first : __hfma2(q, bf2(s.lo), __hfma2(q, bf2(s.hi), __hneg2(first))));
   }
 }
