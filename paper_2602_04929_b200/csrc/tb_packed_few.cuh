@@ -327,7 +327,8 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
               few_second<NP>(zero_second<BITS>(z[2 * m]), zero_second<BITS>(z[2 * m + 1]), a[0][n].v, acc);
               few_second<NP>(zero_second<BITS>(z[2 * m]), zero_second<BITS>(z[2 * m + 1]), a[1][n].v, acc);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) sum[m][n][c] = fmaf(sc[2 * m + (c >> 1)], acc[c], sum[m][n][c]);
+              for (int c = 0; c < 4; ++c)  // rows without one are left alone: an infinite activation would make their 0 no number
+                if (has_second<BITS>(z[2 * m + (c >> 1)])) sum[m][n][c] = fmaf(sc[2 * m + (c >> 1)], acc[c], sum[m][n][c]);
             }
       }
       if (st + p.stages < n_st) {
@@ -365,7 +366,13 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
         few_step<BITS, 0, NT, NP>(w[0], w[1], zero_first<BITS>(z[0]), zero_first<BITS>(z[1]), a, acc);
         if (BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(z[0] | z[1])))
 #pragma unroll
-          for (int n = 0; n < NT; ++n) few_second<NP>(zero_second<BITS>(z[0]), zero_second<BITS>(z[1]), a[n].v, acc[n]);
+          for (int n = 0; n < NT; ++n) {
+            float more[4] = {};
+            few_second<NP>(zero_second<BITS>(z[0]), zero_second<BITS>(z[1]), a[n].v, more);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (has_second<BITS>(z[c >> 1])) acc[n][c] += more[c];
+          }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll

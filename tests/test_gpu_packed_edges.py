@@ -174,6 +174,29 @@ def test_zero_points_far_away(bits, dtype, n_tok):
     pu.near(tb.tb_packed_linear_backward(w, p["dy"].cuda())[0], want, bound + far * (p["dy"].double().abs() @ p["Q"].abs()), "dx")
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("bits,group", [(2, 128), (4, 32), (5, 128), (7, 128)])
+@pytest.mark.parametrize("n_tok", [3, 20, 1100])
+def test_infinite_activations_beside_zero_points_of_every_kind(bits, group, n_tok, dtype):
+    """Rows with zero-points among the codes and rows with others side by side: an infinite activation comes to what the formula says in all."""
+    tb = _tb()
+    p = pu.problem(bits, n_tok, 264, 256, bits, group, dtype)
+    g = torch.Generator().manual_seed(bits)
+    z = p["zeros"].clone()
+    z[::3] = torch.randint(129, 257, z[::3].shape, generator=g, dtype=torch.int32)
+    z[1::9] = torch.randint(-900, -384, z[1::9].shape, generator=g, dtype=torch.int32)
+    p = _with_zero_points(p, z)
+    clean = p["x"].clone()
+    p["x"][0, 17], p["x"][1, 200] = float("inf"), float("-inf")
+    w, _ = pu.on_gpu(tb, p)
+    y = tb.tb_packed_linear(w, p["x"].cuda())[0].cpu().double()
+    for t, j in ((0, 17), (1, 200)):
+        k = p["Q"][:, j]
+        assert torch.isnan(y[t][k == 0]).all() and torch.equal(y[t][k != 0], p["x"][t, j].double() * k[k != 0])
+    want, _, bound = pu.forward64(dict(p, x=clean))
+    pu.near(y[2:], want[2:], bound[2:] + 2.02 * 2.0 ** -8 * (clean.double().abs() @ p["Q"].abs().T)[2:], "y")
+
+
 @pytest.mark.parametrize("rank", [16, 64, 128])
 @pytest.mark.parametrize("n_req", [3, 600])
 @pytest.mark.parametrize("n_tok,rows,d", [(600, 520, 256), (2600, 264, 512)])
