@@ -346,7 +346,8 @@ typedef struct {
  * sum passes the largest float, y is infinite or no number, whatever the scale.
  * A value that is not finite reaches the outputs of its own token alone, and one in an
  * adapter those of its requests.
- * n_tok may be 0.  Workspace: tb_packed_linear_workspace bytes (may be 0). */
+ * n_tok may be 0.  Outputs and workspace share no memory with inputs or one another.
+ * Workspace: tb_packed_linear_workspace bytes (may be 0). */
 size_t tb_packed_linear_workspace(const tb_packed_weight* w, const tb_adapters* adapters,
                                   tb_dtype x_type, long long n_tok);
 tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapters, const void* x,
@@ -362,7 +363,9 @@ tb_status tb_packed_linear(const tb_packed_weight* w, const tb_adapters* adapter
  * that no token has), the same bits on every call.  The input comes as x, in full, or
  * as x_codes and x_scales from tb_checkpoint_pack; xa is the forward pass's.  x, codes
  * and xa may be NULL without dA.  dy [n_tok][d_out] of x_type.  n_tok may be 0, with any
- * array of tokens NULL, dx among them.
+ * array of tokens NULL, dx among them.  Outputs and workspace share no memory with inputs
+ * or one another.  What an infinity comes to in dA and dB is not finite, but may be no
+ * number where the formula has an infinity.
  * In bf16 the weights enter dx as two pieces of bf16, 2^-17 of a weight off in the mean and
  * 2^-13.9 at most. */
 size_t tb_packed_linear_backward_workspace(const tb_packed_weight* w, const tb_adapters* adapters,

@@ -562,6 +562,14 @@ def _packed_call(w, ad, x, side):
     return xt, device
 
 
+def _apart(out, name, *inputs):
+    """Refuses an output of the caller's that shares memory with an input: kernels read the one while they write the other."""
+    lo, hi = out.data_ptr(), out.data_ptr() + out.numel() * out.element_size()
+    for t in inputs:
+        if t is not None and t.data_ptr() < hi and lo < t.data_ptr() + t.numel() * t.element_size():
+            raise ValueError(f"{name} must not share memory with another tensor of the call")
+
+
 def _scratch(query, w, ap, key, x, ws, device):
     """(address, bytes, tensor) of a call's scratch: the caller's, or a new one of the size that its shapes need."""
     if ws is not None:
@@ -581,7 +589,8 @@ def _scratch(query, w, ap, key, x, ws, device):
 
 def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=None, y=None, xa=None):
     """(y, xa): y = x Q^T, plus the adapters' share; xa [n_tok][rank] is x A^T of every token's adapter, which the backward
-    pass takes (None without adapters)."""
+    pass takes (None without adapters).  No autograd graph is recorded: gradients come from tb_packed_linear_backward, which an
+    autograd.Function of the caller's calls with what it kept."""
     xt, device = _packed_call(w, adapters, x, 0)
     n_tok, d_out = x.shape[0], w.widths[1]
     if y is None:
@@ -591,6 +600,7 @@ def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=No
         raise ValueError("y must be [n_tok][d_out]")
     else:
         yp = _here(y, device, x.dtype)
+        _apart(y, "y", x, ws, *(adapters.tensors if adapters is not None else ()), *w.tensors)
     ap, xap, shape = None, None, None
     if adapters is None:
         xa = None
@@ -603,6 +613,7 @@ def tb_packed_linear(w: PackedWeight, x, adapters: Adapters | None = None, ws=No
             raise ValueError("xa must be [n_tok][rank]")
         else:
             xap = _here(xa, device, torch.float32)
+            _apart(xa, "xa", x, y, ws, *adapters.tensors, *w.tensors)
     lib = _lib or load()
     wsp, wsb, keep = _scratch(lib.tb_packed_linear_workspace, w, ap, (0, xt, n_tok, shape), x, ws, device)
     status = lib.tb_packed_linear(w.address, ap, _here(x, device, x.dtype), xt, n_tok, yp, xap, wsp, wsb, _stream())

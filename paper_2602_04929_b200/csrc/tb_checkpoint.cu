@@ -5,7 +5,8 @@
 // such pieces in flight.
 //
 // Packing is bound by its instructions as much as by HBM, about nine a value.  bf16 magnitudes are compared two at a time.  The scale's
-// division is two fused steps on 1 / 127 (exact where nothing underflows).  16384 x 8192, bf16: packing 93 us (4.4 TB/s), unpacking 64.5 us
+// division is a product with 1 / 127 and a correction by its remainder, two fused steps (P. Markstein, Computation of elementary functions
+// on the IBM RISC System/6000 processor, 1990); where nothing underflows it rounds correctly, for every mantissa (tested).  16384 x 8192, bf16: packing 93 us (4.4 TB/s), unpacking 64.5 us
 // (6.4 TB/s, the rate of a copy).
 //
 // The codes are those of the true quotient.  y = x * (1 / scale) is off by less than 2^-14 where |y| <= 127, so rounding it decides

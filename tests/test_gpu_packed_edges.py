@@ -382,3 +382,30 @@ def test_8_bit_form_of_the_widest_token():
         c, k = tb.tb_checkpoint_pack(part)
         assert torch.equal(codes[:, s], c) and torch.equal(scales[:, s.start // 128:-(-s.stop // 128)], k)
         assert torch.equal(back[:, s], tb.tb_checkpoint_unpack(c, k, BF))
+
+
+def test_outputs_that_lie_over_inputs_are_refused():
+    tb = _tb()
+    p = pu.problem(1, 40, 64, 64, 4, 0, BF, 2, 64, [0, 40], [0])
+    w, a = pu.on_gpu(tb, p)
+    x = p["x"].cuda()
+    buf = torch.zeros((80, 64), dtype=BF, device="cuda")
+    low = torch.zeros((80, 64), device="cuda")
+    for call in (lambda: tb.tb_packed_linear(w, x, y=x), lambda: tb.tb_packed_linear(w, buf[20:60], y=buf[:40]),
+                 lambda: tb.tb_packed_linear(w, low[:20].view(BF).view(40, 64), a, xa=low[10:50])):
+        with pytest.raises(ValueError):
+            call()
+    y, _ = tb.tb_packed_linear(w, buf[40:], y=buf[:40])        # side by side is fine
+    assert y.data_ptr() == buf.data_ptr()
+
+
+def test_8_bit_scales_are_correctly_rounded():
+    """max|x| / 127 for all 2^23 mantissas, at three exponents, one beside what underflows: the bits of a float division."""
+    tb = _tb()
+    for e in (127, 253, 33):
+        top = (torch.arange(1 << 23, device="cuda", dtype=torch.int32) | e << 23).view(torch.float32)
+        x = torch.zeros((4096, 2048, 128), device="cuda")
+        x[:, :, 5] = top.view(4096, 2048)
+        _, scales = tb.tb_checkpoint_pack(x.view(4096, -1))
+        want = torch.from_numpy(top.cpu().numpy() / np.float32(127.0))
+        assert torch.equal(scales.view(-1).cpu(), want), e
