@@ -12,8 +12,8 @@
 // buffers, scaled and added to float registers by the epilogue warps while the other buffer fills.  The product so has no rounding
 // but that of float sums.  Backward, a scale belongs to the contraction row, so the weight s (c - z) itself is decoded, as two pieces
 // of bf16 (scale8: 2^-17 of the weight in the mean, 2^-13.9 at most; a single piece would put as large an error on dx as its own rounding
-// does).  Each piece is a stage of its own with the same tokens, twice the products of a single one, and the sum stays in tensor memory
-// to its end, one buffer a tile.
+// does).  Each piece is a stage of its own with the same tokens, twice the products of a single one.  Accumulations end after 2048
+// rows here too: in one sum, 8192 rows put dx 1.5e-5 of its size off, 16384 3.3e-5, all to one side.
 //
 // Adapters.  scale v M, v [tokens][rank] float, joins the sum as further contraction steps: slots of 16 for a run of tokens with one
 // adapter, 16 of its rank and one of two bf16 pieces of scale v (2^-16 of it); tokens outside the run have zeros there.  What is not finite in M goes
@@ -21,16 +21,15 @@
 // tokens, so that it reaches no other token.
 //
 // Roles: warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and
-// scales, then the decode warps (forward two warpgroups, backward four, in turn), then the epilogue (forward eight warps, backward
-// four).  The decode warps have no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor cores,
-// waits for all that its thread has in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Forward,
-// registers are split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).
+// scales, then two warpgroups of decode warps, which take pairs of stages in turn, then eight warps of the epilogue.  The decode warps have
+// no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor cores, waits for all that its thread has
+// in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).
 // Every wait is bounded as in the Hessian kernels.  The MMA warp goes through two stages at a time where it can: its instructions
 // between the MMAs, on a scheduler shared with busy warps, are what limits it.
 //
 // 4096 tokens x 8192 x 8192, 2 bits: 430-440 us, 1.25-1.28 PFLOP/s (a library's bf16 product settles at 1.37 under the power cap);
-// gradient, two products: 4099 tokens, 860-925 us, 1.28-1.19 PFLOP/s, where a single piece of the weights takes 390; 8192 tokens x 4096 x
-// 4096, 4 bits, 426 us, 1.29 PFLOP/s (204).  Bound by the MMA warp's share of its scheduler and, in long runs, by the power cap.  Small work
+// gradient, two products: 4099 tokens, 760-790 us, 1.45-1.39 PFLOP/s, where a single piece of the weights takes 390; 8192 tokens x 4096 x
+// 4096, 4 bits, 371 us, 1.48 PFLOP/s (204).  Bound by the MMA warp's share of its scheduler and, in long runs, by the power cap.  Small work
 // is bound by latency: 64 tokens x 4096 x 4096 takes 13 us, 3 of them the start, 3 until the first words are decoded.
 #pragma once
 
@@ -86,12 +85,12 @@ struct ScalePieces {
     less = bf2(__hfma2(bf2(hi), __float2bfloat162_rn(-0.004150390625f), bf2(lo)));
   }
 };
-template <int PIECE>
-__device__ __forceinline__ void scale8(unsigned (&o)[4], const ScalePieces& s) {
+__device__ __forceinline__ void scale8(unsigned (&o)[4], unsigned (&second)[4], const ScalePieces& s) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const __nv_bfloat162 q = bf2(o[i]), first = __hfma2(q, bf2(s.hi), __hmul2(q, bf2(s.less)));
-    o[i] = bf2(PIECE == 0 ? first : __hfma2(q, bf2(s.lo), __hfma2(q, bf2(s.hi), __hneg2(first))));
+    o[i] = bf2(first);
+    second[i] = bf2(__hfma2(q, bf2(s.lo), __hfma2(q, bf2(s.hi), __hneg2(first))));
   }
 }
 
@@ -100,7 +99,7 @@ __device__ __forceinline__ void sts16(uint32_t addr, const unsigned (&o)[4]) {
 }
 
 // The packed words on their way to the decode warps: 128 columns of the CTA's 128 weight rows (forward, two stages) or of 64 weight
-// rows (backward, two stages, one a piece), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points,
+// rows (backward, a stage for each piece), 16 BITS bytes a row, by TMA, then what belongs to their four runs of 32 columns: zero-points,
 // backward each beside its scale.  A ring of STAGES such units.  Rows of 32, 64 and 128 bytes are swizzled, so that neighbouring threads' rows lie
 // in different banks.
 template <int BITS, bool BACK>
@@ -114,9 +113,8 @@ struct Raw {
     MMA_STAGES = BITS <= 4 ? 6 : 4,  // even: the MMA warp takes two at a time
     ROOM = PT_SMEM - 1024 - 512 - MMA_STAGES * PT_STAGE_BYTES,
     FIT = ROOM / PAD < 8 ? ROOM / PAD : 8,
-    // units go to a warpgroup in turn with another (backward: to two of them, one a piece, in turn with the other two).  A whole number
-    // of turns, so that a slot is always the same ones': waits go by parity, and one that skipped a phase of the barrier that it looks
-    // at would take the phase before for its own
+    // a whole number of turns of the two warpgroups, so that a slot is always the same one's: waits go by parity, and one that skipped a
+    // phase of the barrier that it looks at would take the phase before for its own
     STAGES = FIT / 2 * 2
   };
   static_assert(STAGES >= 2, "the ring holds a unit for every turn");
@@ -134,29 +132,33 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// 64 neighbouring codes of a row into the tile: c - z, or (PIECE) a piece of s (c - z).  SECOND: with the zero-points' second pieces.
-enum { PLAIN = -1 };
-template <int BITS, int C, int PIECE, bool SECOND>
+// 64 neighbouring codes of a row into the tile: c - z, or (SCALED) the pieces of s (c - z), the second into the stage behind.  FAR: with the
+// zero-points' second pieces.
+template <int BITS, int C, bool SCALED, bool FAR>
 __device__ __forceinline__ void decode_codes(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
                                              uint32_t sw) {
   if constexpr (C < 8) {
     unsigned o[4];
     decode8<BITS, 8 * C>(w, zero_first<BITS>(z[C / 4]), o);
-    if constexpr (SECOND)
+    if constexpr (FAR)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = bf2(__hadd2(bf2(o[i]), bf2(zero_second<BITS>(z[C / 4]))));
-    if constexpr (PIECE != PLAIN) scale8<PIECE>(o, s[C / 4]);
+    if constexpr (SCALED) {
+      unsigned second[4];
+      scale8(o, second, s[C / 4]);
+      sts16(row_addr + PT_STAGE_BYTES + ((C ^ sw) << 4), second);
+    }
     sts16(row_addr + ((C ^ sw) << 4), o);
-    decode_codes<BITS, C + 1, PIECE, SECOND>(w, z, s, row_addr, sw);
+    decode_codes<BITS, C + 1, SCALED, FAR>(w, z, s, row_addr, sw);
   }
 }
-template <int BITS, int PIECE>
+template <int BITS, bool SCALED>
 __device__ __forceinline__ void decode_row(const unsigned (&w)[2 * BITS], const unsigned (&z)[2], const ScalePieces (&s)[2], uint32_t row_addr,
                                            uint32_t sw) {
   if (BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(z[0] | z[1])))
-    decode_codes<BITS, 0, PIECE, BITS < 8>(w, z, s, row_addr, sw);
+    decode_codes<BITS, 0, SCALED, BITS < 8>(w, z, s, row_addr, sw);
   else
-    decode_codes<BITS, 0, PIECE, false>(w, z, s, row_addr, sw);
+    decode_codes<BITS, 0, SCALED, false>(w, z, s, row_addr, sw);
 }
 
 __device__ __forceinline__ bool not_finite2(unsigned v) {
@@ -173,15 +175,14 @@ __device__ __forceinline__ unsigned short piece_of(float v, int piece) {
   return *reinterpret_cast<const unsigned short*>(&lo);
 }
 
-template <bool BACK>
-struct Roles {
-  enum { DECODE = BACK ? 4 : 2, EPILOGUE = BACK ? 4 : 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
+// Warpgroups that decode, epilogue warps, the first of these, threads.
+struct R {
+  enum { DECODE = 2, EPILOGUE = 8, EPI0 = 4 + 4 * DECODE, THREADS = 32 * (EPI0 + EPILOGUE) };
 };
 
 template <int BITS, bool BACK>
-__global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+__global__ void __launch_bounds__(R::THREADS, 1) k_packed_tc(const __grid_constant__ PackedTc p, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
   using Ring = Raw<BITS, BACK>;
-  using R = Roles<BACK>;
   constexpr int STAGES = Ring::MMA_STAGES;
   extern __shared__ unsigned char pt_smem_raw[];
   const uint32_t raw = smem_u32(pt_smem_raw);
@@ -216,7 +217,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     }
     for (int s = 0; s < 8; ++s) {
       mbar_init(raw_full(s), 1);
-      mbar_init(raw_empty(s), BACK ? 8 : 4);
+      mbar_init(raw_empty(s), 4);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf_bar(b), 1);
@@ -242,7 +243,6 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
   pdl_trigger();
   const int half_n = p.n_tile >> 1;
   const int n_tiles = p.m_tiles * p.t_tiles * p.splits;
-  const int group = BACK ? p.n_sum : p.w.group;  // columns of a scale that leaves the sum
   struct Tile {
     int m0, t0, split, k0, k1, n_runs, lora;
   };
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
   auto stages_of = [&](const Tile& c) { return (c.k1 - c.k0 + PT_BK - 1) / PT_BK * (BACK ? 2 : 1); };
 
   if (warp < 4) {
-    if (!BACK) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 0 && lane == 0) {
       // ---------------- TMA producer: this CTA's half of the tokens ----------------
       uint32_t it = 0;
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
       const uint64_t a_main = BACK ? smem_desc_mn_sw128(base) : smem_desc_k_sw128(base), a_lora = smem_desc_mn_sw128(base);
       const uint64_t b_main = smem_desc_k_sw128(base + PT_A_BYTES);
       constexpr uint32_t a_step = (BACK ? 2048 : 32) >> 4, l_step = 2048 >> 4, b_step = 32 >> 4;
-      Parts parts(group);
+      Parts parts(p.w.group);
       auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, abort_flag, &g_packed_error); };
       auto acc_free = [&]() {
         const bool got = wait(acce_bar(acc_it & 1u), ((acc_it >> 1) & 1u) ^ 1u);
@@ -318,16 +318,16 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
         const Tile c = tile_of(t);
         const int n_st = stages_of(c);
         int st = 0, left = 0;
-        // accumulations of one length and of whole pairs of stages: nothing to keep but how many pairs are left.  Backward all are: an
-        // accumulation is the tile's, a pair is two pieces, and what lies behind the last row is zeros
-        const int len = BACK ? n_st * PT_BK : parts.part;
-        const bool regular = BACK || (group % len == 0 && c.k0 % len == 0 && c.k1 % len == 0 && len % (2 * PT_BK) == 0 && s % 2 == 0);
+        // accumulations of one length and of whole pairs of stages: nothing to keep but how many pairs are left.  Backward all are: a pair is
+        // two pieces, and what lies behind the last row is zeros
+        const int len = parts.part;
+        const bool regular = BACK || (p.w.group % len == 0 && c.k0 % len == 0 && c.k1 % len == 0 && len % (2 * PT_BK) == 0 && s % 2 == 0);
         if (regular) {
           uint32_t d = 0, more = 0;
           for (; st < n_st; st += 2) {
             if (left == 0) {
               ok = acc_free();
-              left = len / (2 * PT_BK);
+              left = BACK ? min(PT_PART / PT_BK, (n_st - st) / 2) : len / (2 * PT_BK);
               d = tmem_base + (acc_it & 1u) * 256u;
               more = 0;
             }
@@ -347,11 +347,11 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             if (one) {
               four(d, a_main + at + (PT_STAGE_BYTES >> 4), b_main + at + (PT_STAGE_BYTES >> 4), 1);
               umma_commit_pair(empty_bar(s + 1));
-              if (left == 0 && (!BACK || c.lora == 0)) umma_commit_pair(accf_bar(acc_it & 1u));
+              if (left == 0) umma_commit_pair(accf_bar(acc_it & 1u));
             }
             __syncwarp();
             more = 1;
-            if (left == 0 && (!BACK || c.lora == 0)) ++acc_it;
+            if (left == 0) ++acc_it;
             s += 2;
             if (s == STAGES) s = 0, phase ^= 1u;
           }
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
             if (one) umma_commit_pair(empty_bar(s));
             __syncwarp();
           } else {
-            if (!BACK && st == n_st) {  // forward, an accumulation of their own: no scale applies to them
+            if (st == n_st) {  // an accumulation of their own: no scale applies to them
               ok = acc_free();
               if (!ok) break;
             }
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
 #pragma unroll
               for (int kk = 0; kk < PT_BK / 16; ++kk)
                 umma_bf16_pair(tmem_base + (acc_it & 1u) * 256u, a_lora + at + kk * l_step, bd + kk * b_step, id_lora,
-                               !BACK && st == n_st && kk == 0 ? 0u : 1u);
+                               st == n_st && kk == 0 ? 0u : 1u);
               umma_commit_pair(empty_bar(s));
               if (last) umma_commit_pair(accf_bar(acc_it & 1u));
             }
@@ -453,15 +453,14 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     }
   } else if (warp < R::EPI0) {
     // ---------------- decode: operand A of this CTA ----------------
-    if (!BACK) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     const int tid = (threadIdx.x - 128) & 127, turn = (warp - 4) >> 2;  // the warpgroups take turns at the units
     // forward: thread = tile row (a weight row), 64 contraction columns of a stage; backward: 64 weight rows x two halves
     const int my_row = BACK ? tid & 63 : tid;
     const uint32_t row_off = BACK ? (uint32_t)(tid >> 6) * 8192u + (uint32_t)my_row * 128u : (uint32_t)my_row * 128u;
     const uint32_t sw = (uint32_t)(my_row & 7);
     const bool one_sz = p.w.group % 128 == 0;
-    // forward, a unit is two stages of a warpgroup; backward it is one of each of two, and `unit` counts stages: odd ones are second pieces
-    constexpr int PER = BACK ? 1 : 2;
+    constexpr int PER = 2;  // stages of a unit: its two halves, backward its two pieces
     uint32_t it = 0, unit = 0, tiles = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
@@ -478,12 +477,12 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
           it += here;
           continue;
         }
-        const uint32_t in_ring = BACK ? unit >> 1 : unit, rs = in_ring % Ring::STAGES;
-        ok = mbar_wait_warp(raw_full(rs), (in_ring / Ring::STAGES) & 1u, abort_flag, &g_packed_error);
+        const uint32_t rs = unit % Ring::STAGES;
+        ok = mbar_wait_warp(raw_full(rs), (unit / Ring::STAGES) & 1u, abort_flag, &g_packed_error);
         if (!ok) break;
         const unsigned char* q = gen_base + (raw_base - base) + rs * Ring::PAD;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
+        for (int i = 0; i < (BACK ? 1 : PER); ++i) {
           if (i >= here) break;
           // outside the matrix the words are zeros and any zero-point gives finite values, which meet zeros or are not stored
           const int half = BACK ? tid >> 6 : i;  // of the unit's 128 columns
@@ -513,24 +512,22 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
               z[h] = reinterpret_cast<const unsigned*>(q + Ring::Z)[o];
             }
           }
-          if (i == here - 1) {
+          if (BACK || i == here - 1) {
             __syncwarp();
             if (lane == 0) mbar_arrive(raw_empty(rs));
           }
           const int s = it % STAGES;
           ok = mbar_wait_warp(empty_bar(s), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
+          if (BACK && ok) ok = mbar_wait_warp(empty_bar(s + 1), ((it / STAGES) & 1u) ^ 1u, abort_flag, &g_packed_error);
           if (!ok) break;
-          const uint32_t to = base + s * PT_STAGE_BYTES + row_off;
-          if constexpr (!BACK)
-            decode_row<BITS, PLAIN>(w, z, sc, to, sw);
-          else if (turn & 1)
-            decode_row<BITS, 1>(w, z, sc, to, sw);
-          else
-            decode_row<BITS, 0>(w, z, sc, to, sw);
+          decode_row<BITS, BACK>(w, z, sc, base + s * PT_STAGE_BYTES + row_off, sw);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
-          ++it;
+          if (lane == 0) {
+            mbar_arrive_remote_cta(map_to_rank(full_bar(s), 0));
+            if (BACK) mbar_arrive_remote_cta(map_to_rank(full_bar(s + 1), 0));
+          }
+          it += BACK ? 2 : 1;
         }
       }
       // the adapters (where the sum is not split): four slots a stage, slot = (run, 16 of the rank, piece)
@@ -609,15 +606,15 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
     }
   } else {
     // ---------------- epilogue: 128 columns (TMEM lanes), half of the tokens each ----------------
-    if (!BACK) asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
-    const int q = warp & 3, hf = BACK ? 0 : (warp - R::EPI0) >> 2, my_n = BACK ? p.n_tile : half_n;
-    Parts parts(group);
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    const int q = warp & 3, hf = (warp - R::EPI0) >> 2;
+    Parts parts(p.w.group);
     uint32_t acc_it = 0;
     bool ok = true;
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile c = tile_of(t);
       const int col = c.m0 + q * 32 + lane;
-      const int tok0 = c.t0 + hf * half_n, n = min(my_n, p.n_tok - tok0);  // this warp's tokens
+      const int tok0 = c.t0 + hf * half_n, n = min(half_n, p.n_tok - tok0);  // this warp's tokens
       const bool store = col < p.n_cols && n > 0;
       const long long at = (long long)tok0 * p.n_cols + col;
       float* fo = p.part + (long long)c.split * p.n_tok * p.n_cols + at;
@@ -634,64 +631,46 @@ __global__ void __launch_bounds__(Roles<BACK>::THREADS, 1) k_packed_tc(const __g
         if (lane == 0) mbar_arrive_remote_relaxed(map_to_rank(acce_bar(acc_it & 1u), 0));
         ++acc_it;
       };
-      if constexpr (BACK) {
+      float run[128];
+#pragma unroll
+      for (int i = 0; i < 128; ++i) run[i] = 0.0f;
+      if (!BACK) parts.start(c.k0);
+      int k = c.k0;
+      bool lora = false;
+      while (true) {
+        if (k >= c.k1) {
+          if (lora || c.lora == 0) break;
+          lora = true;
+        }
+        float s = 1.0f;
+        if (!BACK && !lora) s = p.st[(long long)parts.g * p.rows_pad + col];
         if (!acc_full()) break;
         const uint32_t taddr = tmem_row + (acc_it & 1u) * 256u;
-        for (int ch = 0; 16 * ch < my_n; ++ch) {
+#pragma unroll
+        for (int ch = 0; ch < 8; ++ch) {
+          if (16 * ch >= half_n) break;
           uint32_t r[16];
           tmem_ld_32x16(taddr + ch * 16, r);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (!store) continue;
-          if (p.part) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (16 * ch + i < n) fo[(long long)(16 * ch + i) * p.n_cols] = __uint_as_float(r[i]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (16 * ch + i < n) bo[(long long)(16 * ch + i) * p.n_cols] = __float2bfloat16(__uint_as_float(r[i]));
-          }
+          for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
         }
         acc_read();
-      } else {
-        float run[128];
+        if (BACK)
+          k += PT_PART;
+        else if (!lora)
+          k = parts.end, parts.next();
+      }
+      if (!ok) break;
+      if (store) {  // (32 bits hold 127 rows of the 2^24 columns that a call may have)
+        if (p.part) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i) run[i] = 0.0f;
-        parts.start(c.k0);
-        int k = c.k0;
-        bool lora = false;
-        while (true) {
-          if (k >= c.k1) {
-            if (lora || c.lora == 0) break;
-            lora = true;
-          }
-          float s = 1.0f;
-          if (!lora) s = p.st[(long long)parts.g * p.rows_pad + col];
-          if (!acc_full()) break;
-          const uint32_t taddr = tmem_row + (acc_it & 1u) * 256u;
+          for (int i = 0; i < 128; ++i)
+            if (i < n) fo[i * p.n_cols] = run[i];
+        } else {
 #pragma unroll
-          for (int ch = 0; ch < 8; ++ch) {
-            if (16 * ch >= half_n) break;
-            uint32_t r[16];
-            tmem_ld_32x16(taddr + ch * 16, r);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < 16; ++i) run[16 * ch + i] = fmaf(s, __uint_as_float(r[i]), run[16 * ch + i]);
-          }
-          acc_read();
-          if (!lora) k = parts.end, parts.next();
-        }
-        if (!ok) break;
-        if (store) {  // (32 bits hold 127 rows of the 2^24 columns that a call may have)
-          if (p.part) {
-#pragma unroll
-            for (int i = 0; i < 128; ++i)
-              if (i < n) fo[i * p.n_cols] = run[i];
-          } else {
-#pragma unroll
-            for (int i = 0; i < 128; ++i)
-              if (i < n) bo[i * p.n_cols] = __float2bfloat16(run[i]);
-          }
+          for (int i = 0; i < 128; ++i)
+            if (i < n) bo[i * p.n_cols] = __float2bfloat16(run[i]);
         }
       }
       if (!store) continue;
@@ -733,13 +712,13 @@ tb_status launch_packed_tc(const PackedTc& p, const CUtensorMap& xmap, const CUt
   if (!configured[dev]) {
     cudaFuncAttributes at;
     TB_CUDA_CHECK(cudaFuncGetAttributes(&at, k_packed_tc<BITS, BACK>));
-    if (!BACK && at.numRegs != 96) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 96 registers a thread has
+    if (at.numRegs != 96) return TB_ERR_CUDA;  // the warpgroups' shares add up to what a launch at 96 registers a thread has
     TB_CUDA_CHECK(cudaFuncSetAttribute(k_packed_tc<BITS, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PT_SMEM));
     configured[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
-  cfg.blockDim = dim3(Roles<BACK>::THREADS);
+  cfg.blockDim = dim3(R::THREADS);
   cfg.dynamicSmemBytes = PT_SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];

@@ -292,6 +292,27 @@ def test_an_infinite_gradient_meets_the_weights(bits, group, n_tok):
     pu.near(dx[3:], want[3:], bound[3:], "dx") if n_tok > 3 else None
 
 
+def test_input_gradient_of_many_rows():
+    """No accumulation of dx is longer than 2048 rows.  The unit drops bits instead of rounding, so errors go to one side: towards 0, at most 2^-23
+    of the sum that a step of 16 rows (of either piece) adds to, which on the way to 2048 rows averages 2/3 of their sum: 2/3 * 256 2^-23 of
+    dx, whatever the number of rows.  Its rounding goes to both sides: over eight million values 1.66e-3 comes to 5.7e-7 in the mean, at most
+    three times that."""
+    tb = _tb()
+    n_tok, rows, d = 4099, 32768, 2048
+    g = torch.Generator(device="cuda").manual_seed(2)
+    words = torch.randint(-1 << 31, 1 << 31, (rows, d // 8), generator=g, device="cuda").to(torch.int32)
+    scales = 0.01 + 0.01 * torch.rand((rows, d // 128), generator=g, device="cuda")
+    zeros = torch.randint(0, 16, (rows, d // 128), generator=g, device="cuda", dtype=torch.int32)
+    codes = ((words.unsqueeze(-1) >> torch.arange(0, 32, 4, device="cuda", dtype=torch.int32)) & 15).view(rows, d)
+    Q = (codes.double() - zeros.repeat_interleave(128, 1)) * scales.double().repeat_interleave(128, 1)
+    dy = torch.randn((n_tok, rows), generator=g, device="cuda").to(BF)
+    dx, _, _ = tb.tb_packed_linear_backward(tb.packed_weight(words, scales, zeros, d, 4, 128), dy)
+    want = dy.double() @ Q
+    shift = ((dx.double() - want) * want.sign()).mean() / want.abs().mean()
+    assert abs(shift.item()) <= 2 / 3 * 256 * 2.0 ** -23 + 3 * 5.7e-7
+    assert tb.tb_device_error_flag() == 0
+
+
 @pytest.mark.parametrize("n_tok,d,rank,n_req", [(16, 524288, 16, 2), (2048, 524288, 64, 2), (5000, 65536, 128, 1), (5000, 65536, 48, 3), (300, 100032, 8, 2), (40, 65536, 128, 7),
                                                 (2600, 10240, 112, 2), (1300, 33344, 40, 5)])
 def test_sums_of_the_narrow_product(n_tok, d, rank, n_req):
