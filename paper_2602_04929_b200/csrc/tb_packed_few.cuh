@@ -70,8 +70,12 @@ template <int BITS, int C, int NT, int NP, int N>
 __device__ __forceinline__ void few_step(const unsigned (&w0)[N], const unsigned (&w1)[N], unsigned z0, unsigned z1, const Acts<NP> (&x)[NT],
                                          float (&acc)[NT][4]) {
   unsigned a[4], b[4];
-  decode8<BITS, 8 * C>(w0, z0, a);
-  decode8<BITS, 8 * C>(w1, z1, b);
+  decode8<BITS, 8 * C>(w0, zero_first<BITS>(z0), a);
+  decode8<BITS, 8 * C>(w1, zero_first<BITS>(z1), b);
+  if constexpr (BITS < 8)  // the zero-points' second pieces: 0 mostly, but a vote and a branch cost more than adding them to eight codes
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      a[i] = bf2(__hadd2(bf2(a[i]), bf2(zero_second<BITS>(z0)))), b[i] = bf2(__hadd2(bf2(b[i]), bf2(zero_second<BITS>(z1))));
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -82,14 +86,6 @@ __device__ __forceinline__ void few_step(const unsigned (&w0)[N], const unsigned
 }
 
 // The zero-points' second pieces, the same for every code of a row: as further weights beside the same activations.
-template <int NP>
-__device__ __forceinline__ void few_second(unsigned z0, unsigned z1, const unsigned (&x)[NP][4], float (&acc)[4]) {
-#pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    mma_few(acc, z0, z1, z0, z1, x[p][0], x[p][1]);
-    mma_few(acc, z0, z1, z0, z1, x[p][2], x[p][3]);
-  }
-}
 template <int NP>
 __device__ __forceinline__ void few_second(unsigned z0, unsigned z1, const unsigned (&x)[NP][8], float (&acc)[4]) {
 #pragma unroll
@@ -363,16 +359,7 @@ __global__ void __launch_bounds__(256, NT * NP == 1 ? 2 : 1) k_packed_few(const 
           z[i] = zero_word(p.w.zeros[sz0 + e * p.w.n_g + gi], BITS);
           s[i] = p.w.scales[sz0 + e * p.w.n_g + gi];
         }
-        few_step<BITS, 0, NT, NP>(w[0], w[1], zero_first<BITS>(z[0]), zero_first<BITS>(z[1]), a, acc);
-        if (BITS < 8 && __any_sync(0xffffffffu, has_second<BITS>(z[0] | z[1])))
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float more[4] = {};
-            few_second<NP>(zero_second<BITS>(z[0]), zero_second<BITS>(z[1]), a[n].v, more);
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (has_second<BITS>(z[c >> 1])) acc[n][c] += more[c];
-          }
+        few_step<BITS, 0, NT, NP>(w[0], w[1], z[0], z[1], a, acc);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
