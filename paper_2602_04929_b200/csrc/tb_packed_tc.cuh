@@ -165,14 +165,12 @@ __device__ __forceinline__ bool not_finite2(unsigned v) {
   return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
 }
 
-// bf16 pieces of v: the value rounded (a finite one to no more than the largest of bf16), and what that leaves rounded, nothing of what
-// is not finite
-__device__ __forceinline__ unsigned short piece_of(float v, int piece) {
-  constexpr float top = 3.38953139e38f;  // (2 - 2^-7) 2^127
-  const __nv_bfloat16 hi = __float2bfloat16(fabsf(v) <= 3.40282347e38f ? fminf(fmaxf(v, -top), top) : v);
-  if (piece == 0) return *reinterpret_cast<const unsigned short*>(&hi);
-  const __nv_bfloat16 lo = __float2bfloat16(rest_of(v, __float_as_uint(__bfloat162float(hi))));
-  return *reinterpret_cast<const unsigned short*>(&lo);
+// A bf16 piece of two values: themselves rounded, or what that leaves rounded, nothing of what is not finite.  TOP: truncated, so that
+// finite values above the largest bf16 stay finite.
+template <bool TOP>
+__device__ __forceinline__ unsigned pieces_of(float lo, float hi, int piece) {
+  const unsigned p = TOP ? first_pieces(lo, hi) : bf2(__floats2bfloat162_rn(lo, hi));
+  return piece == 0 ? p : bf2(__floats2bfloat162_rn(rest_of(lo, p << 16), rest_of(hi, p & 0xffff0000u)));
 }
 
 // Warpgroups that decode, epilogue warps, the first of these, threads.
@@ -578,13 +576,20 @@ __global__ void __launch_bounds__(R::THREADS, 1) k_packed_tc(const __grid_consta
               if (tok >= ru.x && tok < ru.y) {
                 const float f = p.ad.scale[ru.z];
                 const int r0 = (q >> 1) * 16;
+                const float2* low = reinterpret_cast<const float2*>(p.low + (long long)tok * p.ad.rank + r0);
+                float top = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                  const int r = r0 + 2 * i;
-                  if (r < p.ad.rank) {  // rank is a multiple of 8
-                    const float2 v = *reinterpret_cast<const float2*>(p.low + (long long)tok * p.ad.rank + r);
-                    o[i] = (unsigned)piece_of(f * v.x, q & 1) | ((unsigned)piece_of(f * v.y, q & 1) << 16);
+                for (int i = 0; i < 8; ++i)
+                  if (r0 + 2 * i < p.ad.rank) {  // rank is a multiple of 8
+                    const float2 v = low[i];
+                    const float a = f * v.x, b = f * v.y;
+                    top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+                    o[i] = pieces_of<false>(a, b, q & 1);
                   }
+                if (top > 3.38953139e38f) {  // the largest bf16
+#pragma unroll
+                  for (int i = 0; i < 8; ++i)
+                    if (r0 + 2 * i < p.ad.rank) o[i] = pieces_of<true>(f * low[i].x, f * low[i].y, q & 1);
                 }
               }
             }
