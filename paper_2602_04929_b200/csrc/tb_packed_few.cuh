@@ -6,7 +6,8 @@
 // does not matter as long as both operands agree: a lane takes 32 neighbouring codes of a row (BITS words), hence its quad 128 columns,
 // and the same columns of x; 16 codes decode to the eight registers that four MMAs take.  With two and four bits a pair of neighbours
 // in a register is a code of a word's lower half and the one 16 bits above it, so that a mask extracts both, and it is x that is
-// brought into that order, once for all MT tiles.  c - z is exact in bf16; the scale of a row and of the 128 columns multiplies the
+// brought into that order, once for all MT tiles.  c - z is exact in bf16 (zero-points' second pieces, where a warp meets one, are further
+// weights beside the same activations); the scale of a row and of the 128 columns multiplies the
 // sum.  Float activations go through three bf16 pieces, all 24 bits.
 //
 // The words come by TMA, in stages of eight blocks of 128 columns (one for every warp), as many stages ahead as fit beside a second
@@ -14,8 +15,9 @@
 // leave a CTA and a half for every SM; where even 16 rows do not, CTAs of a cluster (cs of them) have a range of blocks each.  The
 // warps' and the CTAs' sums are joined in a fixed order.
 //
-// 1 token: 4096 x 4096, 4 bits, 6.0 us; 8192 x 8192, 2 bits, 13.0 us (17 MB of words and 4 MB of scales, 1.6 TB/s); 64 tokens x 2048 x
-// 2048, 4 bits, 9.1 us.  Decoding bounds it, an instruction for every two codes at half rate, after about 3 us of launch and first loads.
+// 1 token: 4096 x 4096, 4 bits, 6.0 us; 8192 x 8192, 2 bits, 12.9 us (17 MB of words and 4 MB of scales, 1.6 TB/s); 64 tokens x 2048 x
+// 2048, 4 bits, 9.0 us.  Latency bounds it: nothing is saturated (ALU 44 %, issue 1.9 of 4, DRAM 15 %), about 3 us are launch and first
+// loads, and of decoding, an instruction for every two codes at half rate, there are 1.8 us in the 12.9.
 //
 // NARROW: scales of fewer than 128 columns, or a width that is no multiple of 128.  A lane then takes 8 codes of a run of 32.
 #pragma once

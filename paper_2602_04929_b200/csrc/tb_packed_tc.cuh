@@ -23,7 +23,8 @@
 // Roles: warp 0 TMA of the tokens, warp 1 MMA (CTA 0 issues for the pair), warp 2 TMA of the packed words with their zero-points and
 // scales, then two warpgroups of decode warps, which take pairs of stages in turn, then eight warps of the epilogue.  The decode warps have
 // no global loads of their own: fence.proxy.async, which hands a decoded stage to the tensor cores, waits for all that its thread has
-// in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are split 40 / 56 / 56 / 160 / 160 over the five warpgroups of a launch at 96 (no more in sum than the launch has).
+// in flight, and loads of a row by every lane would take the load unit 32 clocks each.  Registers are split 40 / 56 / 56 / 160 / 160 over
+// the five warpgroups of a launch at 96 (no more in sum than the launch has).
 // Every wait is bounded as in the Hessian kernels.  The MMA warp goes through two stages at a time where it can: its instructions
 // between the MMAs, on a scheduler shared with busy warps, are what limits it.
 //
