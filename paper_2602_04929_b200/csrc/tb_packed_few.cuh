@@ -7,8 +7,8 @@
 // and the same columns of x; 16 codes decode to the eight registers that four MMAs take.  With two and four bits a pair of neighbours
 // in a register is a code of a word's lower half and the one 16 bits above it, so that a mask extracts both, and it is x that is
 // brought into that order, once for all MT tiles.  c - z is exact in bf16 (zero-points' second pieces, where a warp meets one, are further
-// weights beside the same activations); the scale of a row and of the 128 columns multiplies the
-// sum.  Float activations go through three bf16 pieces, all 24 bits.
+// weights beside the same activations); the scale of a row and of the 128 columns multiplies the sum.  Float activations go through three
+// bf16 pieces, all 24 bits.
 //
 // The words come by TMA, in stages of eight blocks of 128 columns (one for every warp), as many stages ahead as fit beside a second
 // CTA: a warp that loads its own words has too few bytes in flight for the memory's latency.  A tile has the most rows (16 MT) that

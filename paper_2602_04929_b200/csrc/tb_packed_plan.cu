@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(256) k_packed_join(const float4* part, uint2* 
 }
 
 // Tile and splits by an estimate of the clocks, fitted to sweeps of both (64 to 1999 tokens, widths of 1024 to 8192): a stage of 64
-// columns (backward there are two, one a piece of the weights) costs its decoding, whatever the tile, and a little for every token, a tile 1500 clocks and what its results take, and
-// splits cost writing and adding their float sums.  The adapters' share is further stages of the tile, four slots each (see the
+// columns (backward there are two, one a piece of the weights) costs its decoding, whatever the tile, and a little for every token, a
+// tile 1500 clocks and what its results take, and splits cost writing and adding their float sums.  The adapters' share is further stages of the tile, four slots each (see the
 // kernel), or joins the float sums: 64 tokens of 32 requests, rank 64, 8192 x 512, has 64 such stages and takes 70 us with them, 26 us
 // joined.
 TcPlan packed_tc_plan(const Adapt& ad, int n_tok, int n_cols, int n_sum, bool back) {

@@ -313,6 +313,28 @@ def test_input_gradient_of_many_rows():
     assert tb.tb_device_error_flag() == 0
 
 
+@pytest.mark.parametrize("n_tok,rows,d,bits,group,rank", [(2600, 4104, 512, 4, 128, 24), (5000, 2056, 256, 7, 32, 64), (3000, 6152, 416, 2, 0, 8)])
+def test_input_gradient_of_several_accumulations_with_adapters(n_tok, rows, d, bits, group, rank):
+    """More than 2048 rows, a last accumulation of a few, the adapters' stages behind them, several tiles for every pair of processors."""
+    tb = _tb()
+    p = pu.problem(rank, n_tok, rows, d, bits, group, BF, 3, rank, [5, n_tok // 3, n_tok // 2, n_tok - 7], [2, 0, 1])
+    w, a = pu.on_gpu(tb, p)
+    dy, Q = p["dy"].cuda().double(), p["Q"].cuda()
+    want, size = dy @ Q, dy.abs() @ Q.abs()
+    for i in range(3):
+        m = (pu.owners(p) == i).cuda()
+        A, B, c = p["A"][i].cuda().double(), p["B"][i].cuda().double(), p["scale"][i].double().item()
+        want[m] += c * (dy[m] @ B.T) @ A
+        size[m] += c * (dy[m].abs() @ B.abs().T) @ A.abs()
+    for _ in range(3):
+        dx, _, _ = tb.tb_packed_linear_backward(w, p["dy"].cuda(), a)
+        off = (dx.double() - want).abs()
+        inner = (pu.sum_bound(rows + rank, 1.0, BF) + 2.0 ** -13.9) * size     # float sums, pieces of the adapters' sums, pieces of the weights
+        assert (off <= inner + pu.HALF_STEP[BF] * (want.abs() + inner)).all()
+        assert float((dx.double() - want).norm() / want.norm()) <= 2.0 ** -9
+        assert tb.tb_device_error_flag() == 0
+
+
 @pytest.mark.parametrize("n_tok,d,rank,n_req", [(16, 524288, 16, 2), (2048, 524288, 64, 2), (5000, 65536, 128, 1), (5000, 65536, 48, 3), (300, 100032, 8, 2), (40, 65536, 128, 7),
                                                 (2600, 10240, 112, 2), (1300, 33344, 40, 5)])
 def test_sums_of_the_narrow_product(n_tok, d, rank, n_req):
